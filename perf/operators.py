@@ -84,7 +84,8 @@ def draw(rng):
         c["tau"] = round(rng.uniform(0.5, 3.0), 3)
         if kind != "topk":
             c["tail"] = rng.random() < 0.5
-            c["live"] = rng.choice([1.0, 0.7])
+        if kind in ("train", "backward"):
+            c["live"] = rng.choice([1.0, 0.7])  # the others carry no weight
     return c
 
 
