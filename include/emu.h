@@ -13,6 +13,10 @@
  *   emu_reshard         execute the map: source shard set -> destination shard set
  *   emu_pack_buckets    concatenate one side's shards per rank into fixed-size contiguous buckets
  *   emu_unpack_buckets  the inverse, on the receiver side
+ * and, on the logits that the LM head of a layout yields, what the stages around it do with them:
+ *   emu_logits_constrain  penalties, biases and grammar masks ahead of sampling
+ *   emu_logits_topk       the k largest log-probabilities of every row
+ *   emu_distill           distillation from a teacher's top logits, with emu_distill_backward
  *
  * Conventions (the paper fixes none of them; these are the readings the library implements):
  *   - Megatron-style sharding: q/k/v and gate/up column-parallel, o and down row-parallel,
@@ -365,6 +369,115 @@ int emu_unpack_buckets(emu_plan_t plan, const void* d_workspace, int32_t side, u
 int emu_check_tables(emu_plan_t plan, const uint64_t* src_ptrs, const uint64_t* dst_ptrs);
 int emu_check_bucket_tables(emu_plan_t plan, int32_t side, uint64_t bucket_bytes, const uint64_t* tensor_ptrs,
                             const uint64_t* bucket_ptrs);
+
+/* ------------------------------------------------------------------------------------------------
+ * Operators on the logits of a vocab-parallel LM head: what a generation stage samples from, what a teacher
+ * hands on and what a student learns from, read in the shards that a layout's LM head yields. A Split or Merge
+ * changes how the vocabulary is cut, not the model (section 5.2 (a)/(b); section 6.2, preserving training
+ * semantics): every result is the same, bit for bit, whatever tp and the padding are.
+ *
+ *   - Logits of layout *layout (vocabulary V, padded to Vp columns): tp shards, shard t holding columns
+ *     [t*Vp/tp, (t+1)*Vp/tp) of every row. The layout's dtype is its weights'; the logits have their own.
+ *     Columns from V on (pad rows of the LM head) are never read; output shards get the value stated there.
+ *   - Shard addresses come in a HOST array, which the call copies (logits are new each step; a device table
+ *     would need an upload each time). A shard starts at any multiple of its element size; rows are
+ *     row_stride elements apart, the same in all shards of one set. Columns past Vp/tp are not touched.
+ *   - All other operands are device arrays, 4-byte aligned. Operands that say "or NULL" may be absent.
+ *   - An output set may be the input set itself (same dtype, stride and addresses). Otherwise the buffers of a
+ *     call must not overlap (undefined behaviour).
+ *   - Sums, softmax statistics and losses are fp32 or wider, rounded to the output's type once. No result
+ *     depends on the order of atomics.
+ *   - Limits: tp <= 64, V <= 2^22, rows <= 2^31 - 1 (EMU_ERR_UNSUPPORTED); zero rows are a call that does nothing.
+ *   - A workspace (emu_logits_workspace) holds what the workgroups of one call hand each other. It needs no
+ *     initial contents and keeps nothing for later calls. Two calls that may run at the same time need two. */
+
+typedef struct {
+  const emu_layout_t* layout;
+  int32_t dtype;               /* emu_dtype of the logits */
+  int32_t n_shards;            /* entries of shards: the layout's tp */
+  int64_t rows, row_stride;    /* row_stride in elements, >= Vp/tp */
+  void* const* shards;         /* HOST array of device addresses */
+} emu_logits_t;
+
+/* What constrains one step's logits, row by row. */
+typedef struct {
+  const int32_t* tokens;       /* or NULL: [rows][tokens_stride], row r's sequence so far */
+  int64_t tokens_stride;
+  int32_t tokens_cols;         /* a row's capacity, <= tokens_stride */
+  int32_t n_masks;
+  const int32_t* seq_len;      /* [rows] tokens of row r that count; needed with tokens */
+  const int32_t* prompt_len;   /* or NULL (all 0): the first prompt_len[r] of them are the prompt */
+  const float* repetition;     /* or NULL: theta[rows], > 0 */
+  const float* frequency;      /* or NULL: alpha_f[rows] */
+  const float* presence;       /* or NULL: alpha_p[rows] */
+  const int32_t* bias_first;   /* or NULL: [rows + 1], row r's biases are entries [bias_first[r], bias_first[r+1]) */
+  const int32_t* bias_token;   /* [n_bias] */
+  const float* bias_value;     /* [n_bias] */
+  int64_t n_bias;
+  const int32_t* mask;         /* or NULL: [n_masks][mask_stride] words, bit v % 32 of word v / 32 set: v allowed */
+  int64_t mask_stride;         /* in words, >= ceil(V / 32) */
+  const int32_t* mask_row;     /* or NULL (row r has mask r, n_masks == rows): row r's mask, none if < 0 */
+} emu_constraints_t;
+
+/* A teacher's top logits per row. */
+typedef struct {
+  int32_t k;                   /* 1 .. 256 entries per row */
+  int32_t tail;                /* 0: the k values are the teacher's whole distribution, up to a constant per row;
+                                  1: they are log-probabilities, what is missing to 1 lies outside the list */
+  float temperature;           /* tau of the student's softmax, > 0 (the teacher's values already hold theirs) */
+  const int32_t* index;        /* [rows][index_stride] columns; entries outside [0, V) are skipped */
+  int64_t index_stride;        /* >= k */
+  const float* value;          /* [rows][value_stride] */
+  int64_t value_stride;        /* >= k */
+  const float* weight;         /* or NULL (all 1): w[rows]. A row of weight 0 is not read */
+} emu_teacher_t;
+
+/* Workspace bytes that emu_logits_topk (k >= 1) or emu_distill and emu_distill_backward (k == 0) need for these
+ * logits. Depends on dtype, rows and V only. Host only. */
+int emu_logits_workspace(const emu_logits_t* logits, int32_t k, uint64_t* bytes);
+
+/* Penalties for repeated tokens, biases and grammar masks. For column v < V of row r, with x the logit, c how
+ * often v occurs in tokens[prompt_len, seq_len) and s whether it occurs in tokens[0, seq_len):
+ *   x1 = s ? (x > 0 ? x / theta : x * theta) : x
+ *   x2 = x1 - (alpha_f * c + alpha_p * (c > 0))
+ *   x3 = x2 + the sum of v's biases, in list order
+ *   out = allowed by row r's mask ? x3 : -infinity
+ * and -infinity in every column from V on, so that no pad token is ever sampled. Tokens and biased tokens
+ * outside [0, V) are skipped, lengths are cut to [0, tokens_cols], list ends to [0, n_bias], and a mask_row
+ * >= n_masks counts as none. A mask that allows nothing leaves a row of -infinity. A forbidden NaN becomes
+ * -infinity. out may have the other dtype (then not in place). */
+int emu_logits_constrain(const emu_logits_t* in, const emu_logits_t* out, const emu_constraints_t* constraints,
+                         void* hip_stream);
+
+/* The k largest logits of every row (1 <= k <= 64, k <= V): d_index[rows][k] their columns, d_logprob[rows][k] their
+ * log-probabilities x/tau - lse, and d_lse[rows] (or NULL) lse = log sum exp(x/tau) over the V columns. In
+ * descending order, equal logits in ascending column order (-0 equals 0). -infinity and NaN are never chosen:
+ * where fewer than k are left, index -1 and log-probability -infinity follow. A row that holds a NaN or +infinity
+ * has NaN for its lse and log-probabilities; one that holds -infinity alone has lse -infinity. */
+int emu_logits_topk(const emu_logits_t* in, int32_t k, float temperature, int32_t* d_index, float* d_logprob,
+                    float* d_lse, void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* Distillation from a teacher's top logits: the KL divergence from the teacher's distribution p to the
+ * student's q = softmax(z / tau) over the V columns. With J the row's entries inside [0, V):
+ *   tail 0: p = softmax of the values over J;  L = sum_J p_j (log p_j - log q_j)
+ *           dL/dz_v = (q_v - p_v) / tau
+ *   tail 1: p_j = exp(value), p_R = max(0, 1 - sum_J p_j), q_R the sum of q outside J;
+ *           L = sum_J p_j (log p_j - log q_j) + p_R (log p_R - log q_R)
+ *           dL/dz_v = (q_v - p_v) / tau inside J, q_v (1 - p_R / q_R) / tau outside
+ * Terms with p = 0 are 0. A column listed twice holds the sum of its entries' probabilities. With tail 0 a row
+ * without an entry, or whose values are all -infinity, has L = 0 and gradient 0. Where p > 0 meets q = 0, L is
+ * +infinity and the gradient keeps its finite part (q_R = 0: the factor outside J is 1); against q_R = 0 a p_R below
+ * 2^-20, which the rounding of fp32 log-probabilities leaves, counts as 0.
+ * d_loss[r] = w_r L_r. With grad (or NULL), its shards get w_r dL/dz, and 0 in every column from V on. d_stats
+ * [rows][4], 16-byte aligned: lse of z/tau, the factor 1 - p_R/q_R (1 without a tail), the row's largest logit m and
+ * sum exp((z - m)/tau). A row with w_r = 0 has loss and gradient 0, is not read, and has NaN for its statistics. */
+int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float* d_loss, float* d_stats,
+                const emu_logits_t* grad, void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* The gradient alone, from the statistics that emu_distill left for the same logits, teacher, tail and
+ * temperature: grad = w_r dL/dz, where w (teacher->weight) is now the gradient that reaches row r's loss L_r. */
+int emu_distill_backward(const emu_logits_t* student, const emu_teacher_t* teacher, const float* d_stats,
+                         const emu_logits_t* grad, void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Transition-DAG planner (host only). From a current to a target plan of several model-stages: the

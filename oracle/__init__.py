@@ -28,6 +28,7 @@ Modules:
   buckets  -- per-rank byte streams, bucket pack and unpack
   coords   -- per-element coordinate formulas (pure Python) used by the brute-force pins
   convert  -- fp32 <-> bf16 conversion for the weight-synchronising reshard (round to nearest even)
+  logits   -- constraints, top log-probabilities and distillation on an LM head's logits
 """
 
 from .model import (  # noqa: F401
@@ -39,3 +40,4 @@ from .sharding import (  # noqa: F401
 )
 from .buckets import stream_bytes, bucket_count, pack, unpack  # noqa: F401
 from .convert import convert, f32_to_bf16, bf16_to_f32  # noqa: F401
+from . import logits  # noqa: F401

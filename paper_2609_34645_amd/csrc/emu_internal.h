@@ -150,6 +150,7 @@ bool chunks_realign(const SideInfo& s, uint64_t B, bool unpack);
 LaunchRule bucket_rule(const SideInfo& s, uint64_t B, bool unpack);  // the tile-per-workgroup kernel
 
 uint64_t next_plan_id();
+int64_t padded_vocab(const emu_layout_t& l);  // columns of the LM head's logits, pads included
 
 // errors.cpp-style helpers (defined in emu_plan.cpp)
 int fail(int code, const char* fmt, ...);

@@ -121,7 +121,7 @@ static int check_layout(const emu_layout_t* l) {
   return EMU_OK;
 }
 
-static int64_t padded_vocab(const emu_layout_t& l) {
+int64_t padded_vocab(const emu_layout_t& l) {
   int64_t V = l.model.vocab;
   if (l.vocab_pad_multiple == 0) return V;
   int64_t q = int64_t(l.tp) * l.vocab_pad_multiple;

@@ -1,7 +1,7 @@
 """Python binding of libemu.so (the EMU Split/Merge reshard, C ABI in include/emu.h).
 
-Argument marshalling only: every step of the reshard and of bucket pack/unpack runs in the library's
-HIP kernels. PyTorch provides device memory, pointer tables and streams. There is no fallback: if the
+Argument marshalling only: every step of the reshard, of bucket pack/unpack and of the operators on an LM
+head's logits runs in the library's HIP kernels. PyTorch provides device memory, pointer tables and streams. There is no fallback: if the
 library is not built, :func:`load` raises.
 
 Typical use::
@@ -12,6 +12,11 @@ Typical use::
     ws = plan.workspace()                      # uploads the plan tables to a fresh device buffer
     S = plan.alloc(0); D = plan.alloc(1)       # one buffer per rank, tensors as views
     plan.reshard(ws, S.ptrs, D.ptrs)           # enqueued on torch's current stream
+
+    logits = LogitShards(dst, shards)          # what the destination layout's LM head yields, one shard per TP rank
+    constrain_logits(logits, tokens=tokens, seq_len=n, repetition=theta, mask=grammar)
+    index, logprob, lse = top_logprobs(logits, 64)
+    loss, stats = distill_loss(student, index, logprob, weight=w, grad=grad)
 """
 from __future__ import annotations
 
@@ -113,6 +118,26 @@ class c_dag_info(ctypes.Structure):
                 ("n_gpu_entries", ctypes.c_int32), ("l_tran_s", ctypes.c_double), ("plan_ms", ctypes.c_double)]
 
 
+class c_logits(ctypes.Structure):
+    _fields_ = [("layout", ctypes.POINTER(c_layout)), ("dtype", ctypes.c_int32), ("n_shards", ctypes.c_int32),
+                ("rows", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("shards", ctypes.POINTER(ctypes.c_void_p))]
+
+
+class c_constraints(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("tokens_stride", ctypes.c_int64), ("tokens_cols", ctypes.c_int32),
+                ("n_masks", ctypes.c_int32), ("seq_len", ctypes.c_void_p), ("prompt_len", ctypes.c_void_p),
+                ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                ("bias_first", ctypes.c_void_p), ("bias_token", ctypes.c_void_p), ("bias_value", ctypes.c_void_p),
+                ("n_bias", ctypes.c_int64), ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_int64),
+                ("mask_row", ctypes.c_void_p)]
+
+
+class c_teacher(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_int32), ("tail", ctypes.c_int32), ("temperature", ctypes.c_float),
+                ("index", ctypes.c_void_p), ("index_stride", ctypes.c_int64), ("value", ctypes.c_void_p),
+                ("value_stride", ctypes.c_int64), ("weight", ctypes.c_void_p)]
+
+
 class EmuError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{STATUS.get(code, code)}: {msg}")
@@ -120,12 +145,12 @@ class EmuError(RuntimeError):
 
 
 _lib = None
-_raw_stream = _current_device = _int64 = None  # torch's, set by load()
+_raw_stream = _current_device = _int64 = _int32 = _float32 = _bfloat16 = None  # torch's, set by load()
 
 
 def load(path: str = LIB_PATH):
     """Load libemu.so (once). Raises if it has not been built: there is no other implementation."""
-    global _lib, _raw_stream, _current_device, _int64
+    global _lib, _raw_stream, _current_device, _int64, _int32, _float32, _bfloat16
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
@@ -137,7 +162,7 @@ def load(path: str = LIB_PATH):
     # torch's runtime is the one to share.
     import torch
     lib = ctypes.CDLL(path)
-    _int64 = torch.int64
+    _int64, _int32, _float32, _bfloat16 = torch.int64, torch.int32, torch.float32, torch.bfloat16
     if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice"):
         _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     P, V, I32, I64, U64 = ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
@@ -170,6 +195,11 @@ def load(path: str = LIB_PATH):
         "emu_unpack_buckets": ([P, V, I32, U64, V, V, V], ctypes.c_int),
         "emu_check_tables": ([P, ctypes.POINTER(U64), ctypes.POINTER(U64)], ctypes.c_int),
         "emu_check_bucket_tables": ([P, I32, U64, ctypes.POINTER(U64), ctypes.POINTER(U64)], ctypes.c_int),
+        "emu_logits_workspace": ([V, I32, V], ctypes.c_int),
+        "emu_logits_constrain": ([V, V, V, V], ctypes.c_int),
+        "emu_logits_topk": ([V, I32, ctypes.c_float, V, V, V, V, U64, V], ctypes.c_int),
+        "emu_distill": ([V, V, V, V, V, V, U64, V], ctypes.c_int),
+        "emu_distill_backward": ([V, V, V, V, V, U64, V], ctypes.c_int),
         "emu_dag_plan": ([ctypes.POINTER(c_stage_transition), I32, ctypes.POINTER(c_link_model), ctypes.POINTER(P)],
                          ctypes.c_int),
         "emu_dag_free": ([P], ctypes.c_int),
@@ -621,6 +651,208 @@ def ptr_table(tensors, device=None):
     if bad:
         raise EmuError(-7, f"tensors {bad[:4]} are not 16-byte aligned")
     return torch.tensor(addrs, dtype=torch.int64, device=device or "cuda")
+
+
+# ----------------------------------------------------------------------------------------------------
+# operators on the logits of a vocab-parallel LM head
+# ----------------------------------------------------------------------------------------------------
+
+def shard_columns(layout: Layout) -> int:
+    """Columns of one TP rank's logits: the layout's vocabulary, padded, over tp."""
+    return _head(layout)[1]
+
+
+def _head(layout):
+    """(C layout, columns per shard), kept with the layout, which never changes."""
+    head = layout.__dict__.get("_head")
+    if head is None:
+        c = layout.c()
+        check(load().emu_layout_check(ctypes.byref(c)))
+        q = layout.tp * layout.pad
+        head = (c, (-(-layout.model.vocab // q) * q if q else layout.model.vocab) // layout.tp)
+        object.__setattr__(layout, "_head", head)
+    return head
+
+
+class LogitShards:
+    """The logits that the LM head of ``layout`` yields: ``tensors[t]`` is TP rank t's [rows, shard_columns(layout)]
+    bf16 or fp32 device tensor. Rows may be strided (views of a wider matrix), elements of a row may not; all
+    shards have one dtype and one row stride."""
+
+    def __init__(self, layout: Layout, tensors):
+        c, cols = _head(layout)
+        tensors = list(tensors)
+        if len(tensors) != layout.tp:
+            raise ValueError(f"{len(tensors)} shards, the layout has tp={layout.tp}")
+        first = tensors[0]
+        shape, dtype = first.shape, first.dtype
+        if len(shape) != 2 or shape[1] != cols:
+            raise ValueError(f"a shard is [rows, {cols}], not {list(shape)}")
+        code = BF16 if dtype is _bfloat16 else FP32 if dtype is _float32 else None
+        if code is None:
+            raise ValueError(f"logits must be bfloat16 or float32, not {dtype}")
+        rows = shape[0]
+        stride = first.stride(0) if rows > 1 else max(cols, first.stride(0))
+        for t in tensors:
+            if t.shape != shape or t.dtype is not dtype or (rows > 1 and t.stride(0) != stride):
+                raise ValueError("shards must have one shape, dtype and row stride")
+            if cols > 1 and t.stride(1) != 1:
+                raise ValueError("the elements of a row must be adjacent")
+        _on_device(*tensors)
+        self.layout, self.tensors, self.rows, self.dtype = layout, tensors, rows, dtype
+        self._ptrs = (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+        self._c = c_logits(ctypes.pointer(c), code, len(tensors), rows, stride, self._ptrs)
+        self.ref = ctypes.addressof(self._c)
+
+    @classmethod
+    def alloc(cls, layout: Layout, rows: int, dtype, device=None):
+        """New shards, 16-byte aligned, uninitialised."""
+        import torch
+
+        cols = shard_columns(layout)
+        return cls(layout, [torch.empty(rows, cols, dtype=dtype, device=device or "cuda") for _ in range(layout.tp)])
+
+    def workspace(self, k: int = 0, stream=None):
+        """(tensor or None, bytes) of a workspace for ``top_logprobs`` (k >= 1) or the distillation calls (k = 0)."""
+        n = ctypes.c_uint64()
+        check(load().emu_logits_workspace(self.ref, k, ctypes.addressof(n)))
+        return (_empty((n.value,), _uint8(), self.tensors[0], stream) if n.value else None), n.value
+
+
+def _on_device(*tensors):
+    """Every tensor on the current device: the calls launch there."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise ValueError("not a device tensor")
+    current = _current_device() if _current_device is not None else None
+    for t in tensors:
+        if t is not None and current is not None and t.get_device() != current:
+            raise ValueError(f"a tensor on device {t.get_device()}, the current device is {current}")
+
+
+def _operand(t, name, dtype, *shape):
+    """The address of an optional operand of the given type; a None in shape: any size. Rows may be strided."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {list(t.shape)}, expected {['*' if n is None else n for n in shape]}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: elements must be adjacent")
+    return t.data_ptr()
+
+
+def _row_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _empty(shape, dtype, like, stream):
+    """An uninitialised tensor from the pool of the stream that the call runs on."""
+    import torch
+
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def constrain_logits(logits: LogitShards, out: LogitShards = None, tokens=None, seq_len=None, prompt_len=None,
+                     repetition=None, frequency=None, presence=None, bias=None, mask=None, mask_row=None,
+                     stream=None) -> LogitShards:
+    """``emu_logits_constrain``: penalties for repeated tokens, biases and grammar masks, into ``out`` (default: in
+    place). tokens int32 [rows, capacity] with seq_len int32 [rows] and optionally prompt_len int32 [rows]; repetition,
+    frequency, presence fp32 [rows]; bias = (first int32 [rows + 1], token int32 [n], value fp32 [n]); mask
+    int32 [n, words], one per row or chosen by mask_row int32 [rows] (negative: none)."""
+    rows, i32, f32 = logits.rows, _int32, _float32
+    out = logits if out is None else out
+    c = c_constraints()
+    if tokens is not None:
+        c.tokens = _operand(tokens, "tokens", i32, rows, None)
+        c.tokens_cols, c.tokens_stride = tokens.shape[1], _row_stride(tokens)
+        c.seq_len = _operand(seq_len, "seq_len", i32, rows)
+        c.prompt_len = _operand(prompt_len, "prompt_len", i32, rows)
+        if tokens.shape[1] == 0:
+            c.tokens = None
+    elif seq_len is not None or prompt_len is not None:
+        raise ValueError("lengths without tokens")
+    c.repetition = _operand(repetition, "repetition", f32, rows)
+    c.frequency = _operand(frequency, "frequency", f32, rows)
+    c.presence = _operand(presence, "presence", f32, rows)
+    first = token = value = None
+    if bias is not None:
+        first, token, value = bias
+        n = c.n_bias = token.shape[0]
+        c.bias_first = _operand(first, "bias first", i32, rows + 1)
+        c.bias_token, c.bias_value = _operand(token, "bias token", i32, n), _operand(value, "bias value", f32, n)
+        if n == 0:
+            c.bias_first = None
+    if mask is not None:
+        c.mask = _operand(mask, "mask", i32, None if mask_row is not None else rows, None)
+        c.n_masks, c.mask_stride = mask.shape[0], _row_stride(mask)
+        c.mask_row = _operand(mask_row, "mask_row", i32, rows)
+        if mask.shape[1] * 32 < logits.layout.model.vocab:
+            raise ValueError(f"mask rows of {mask.shape[1]} words are short of {logits.layout.model.vocab} tokens")
+        if mask.shape[0] == 0:
+            c.mask = None
+    elif mask_row is not None:
+        raise ValueError("mask_row without mask")
+    _on_device(tokens, seq_len, prompt_len, repetition, frequency, presence, first, token, value, mask, mask_row)
+    check(load().emu_logits_constrain(logits.ref, out.ref, ctypes.addressof(c), _stream_handle(stream)))
+    return out
+
+
+def top_logprobs(logits: LogitShards, k: int, temperature: float = 1.0, stream=None):
+    """``emu_logits_topk``: (index int32 [rows, k], logprob fp32 [rows, k], lse fp32 [rows]) of the k largest logits
+    of every row, in descending order."""
+    ws, n = logits.workspace(k, stream)
+    like = logits.tensors[0]
+    index = _empty((logits.rows, k), _int32, like, stream)
+    logprob = _empty((logits.rows, k), _float32, like, stream)
+    lse = _empty((logits.rows,), _float32, like, stream)
+    check(load().emu_logits_topk(logits.ref, k, temperature, index.data_ptr(), logprob.data_ptr(), lse.data_ptr(),
+                                 None if ws is None else ws.data_ptr(), n, _stream_handle(stream)))
+    return index, logprob, lse
+
+
+def _teacher(logits, index, value, weight, name, temperature, tail):
+    rows, k = logits.rows, index.shape[-1]
+    c = c_teacher(k, 1 if tail else 0, temperature, _operand(index, "index", _int32, rows, k), _row_stride(index),
+                  _operand(value, "teacher", _float32, rows, k), _row_stride(value),
+                  _operand(weight, name, _float32, rows))
+    _on_device(index, value, weight)
+    return c
+
+
+def distill_loss(logits: LogitShards, index, teacher, weight=None, temperature: float = 1.0, tail: bool = False,
+                 grad: LogitShards = None, stream=None):
+    """``emu_distill``: the weighted KL divergence of every row from a teacher's top logits (index int32 [rows, k],
+    teacher fp32 [rows, k], as ``top_logprobs`` gives them) to the student's softmax at ``temperature``. Returns
+    (loss fp32 [rows], stats fp32 [rows, 4]); with ``grad`` also writes the gradient of the losses' sum with respect to
+    the logits into its shards (which may be the logits themselves)."""
+    c = _teacher(logits, index, teacher, weight, "weight", temperature, tail)
+    ws, n = logits.workspace(0, stream)
+    loss = _empty((logits.rows,), _float32, logits.tensors[0], stream)
+    stats = _empty((logits.rows, 4), _float32, logits.tensors[0], stream)
+    check(load().emu_distill(logits.ref, ctypes.addressof(c), loss.data_ptr(), stats.data_ptr(),
+                             None if grad is None else grad.ref, None if ws is None else ws.data_ptr(), n,
+                             _stream_handle(stream)))
+    return loss, stats
+
+
+def distill_backward(logits: LogitShards, index, teacher, stats, grad_loss, grad: LogitShards,
+                     temperature: float = 1.0, tail: bool = False, stream=None) -> LogitShards:
+    """``emu_distill_backward``: the gradient with respect to the logits, from the statistics of ``distill_loss`` and the
+    gradient grad_loss fp32 [rows] of every row's unweighted loss, into ``grad`` (which may be the logits)."""
+    c = _teacher(logits, index, teacher, grad_loss, "grad_loss", temperature, tail)
+    stats_ptr = _operand(stats, "stats", _float32, logits.rows, 4)
+    if logits.rows > 1 and stats.stride(0) != 4:
+        raise ValueError("stats must be contiguous")
+    _on_device(stats)
+    ws, n = logits.workspace(0, stream)
+    check(load().emu_distill_backward(logits.ref, ctypes.addressof(c), stats_ptr, grad.ref,
+                                      None if ws is None else ws.data_ptr(), n, _stream_handle(stream)))
+    return grad
 
 
 # ----------------------------------------------------------------------------------------------------

@@ -1,0 +1,165 @@
+"""What the logits operators refuse, before anything reaches a GPU: the C calls' checks on made-up addresses, and the
+binding's checks of shapes and types."""
+import ctypes
+
+import pytest
+
+from paper_2609_34645_amd import emu
+
+MODEL = emu.Model(2, 256, 8, 64, 8, 512, 1000)
+LAY = emu.Layout(MODEL, 2, 1)
+ADDRESS = 1 << 20  # never dereferenced: every call here is refused on the host
+
+
+def c_set(layout=LAY, dtype=emu.BF16, rows=4, stride=500, shards=None, n=None):
+    shards = [ADDRESS] * layout.tp if shards is None else shards
+    ptrs = (ctypes.c_void_p * max(1, len(shards)))(*shards)
+    return emu.c_logits(ctypes.pointer(layout.c()), dtype, len(shards) if n is None else n, rows, stride, ptrs)
+
+
+def code(call, *args):
+    rc = getattr(emu.load(), call)(*[ctypes.addressof(a) if isinstance(a, ctypes.Structure) else a for a in args])
+    if rc:
+        assert emu.load().emu_last_error().decode()
+    return emu.STATUS[rc]
+
+
+def topk(l, k=4, tau=1.0, index=ADDRESS, logprob=ADDRESS, lse=ADDRESS, ws=ADDRESS, n=1 << 40):
+    return code("emu_logits_topk", l, k, tau, index, logprob, lse, ws, n, None)
+
+
+def c_teacher(**more):
+    a = dict(k=8, tail=0, temperature=1.0, index=ADDRESS, index_stride=8, value=ADDRESS, value_stride=8, weight=None)
+    a.update(more)
+    return emu.c_teacher(*[a[f] for f, _ in emu.c_teacher._fields_])
+
+
+def distill(l, te, loss=ADDRESS, stats=ADDRESS, grad=None):
+    return code("emu_distill", l, te, loss, stats, grad, ADDRESS, 1 << 40, None)
+
+
+@pytest.mark.parametrize("want,made", [
+    ("EMU_ERR_LAYOUT", dict(layout=emu.Layout(MODEL, 3, 1))),
+    ("EMU_ERR_ARG", dict(dtype=7)),
+    ("EMU_ERR_ARG", dict(shards=[ADDRESS])),
+    ("EMU_ERR_ARG", dict(rows=-1)),
+    ("EMU_ERR_UNSUPPORTED", dict(rows=1 << 31)),
+    ("EMU_ERR_ARG", dict(stride=499)),
+    ("EMU_ERR_ARG", dict(stride=1 << 41)),
+    ("EMU_ERR_NULL", dict(shards=[ADDRESS, None])),
+    ("EMU_ERR_ALIGN", dict(shards=[ADDRESS, ADDRESS + 1])),
+    ("EMU_ERR_ALIGN", dict(dtype=emu.FP32, shards=[ADDRESS, ADDRESS + 2])),
+    ("EMU_ERR_UNSUPPORTED", dict(layout=emu.Layout(emu.Model(2, 256, 128, 64, 128, 512, 1280), 128, 1), stride=10)),
+    ("EMU_ERR_UNSUPPORTED", dict(layout=emu.Layout(emu.Model(2, 256, 8, 64, 8, 512, (1 << 22) + 1), 1, 1), stride=1 << 23)),
+])
+def test_every_call_refuses_the_set(want, made):
+    bad, good = c_set(**made), c_set()
+    assert topk(bad) == want
+    assert distill(bad, c_teacher()) == want
+    assert code("emu_distill_backward", bad, c_teacher(), ADDRESS, good, ADDRESS, 1 << 40, None) == want
+    assert code("emu_distill_backward", good, c_teacher(), ADDRESS, bad, ADDRESS, 1 << 40, None) in (want, "EMU_ERR_MISMATCH")
+    assert code("emu_logits_constrain", bad, good, emu.c_constraints(), None) == want
+    n = ctypes.c_uint64()
+    assert code("emu_logits_workspace", bad, 0, ctypes.addressof(n)) == want
+
+
+def test_outputs_must_be_the_inputs_kin():
+    good, c = c_set(), emu.c_constraints()
+    assert code("emu_logits_constrain", good, c_set(rows=5), c, None) == "EMU_ERR_MISMATCH"
+    assert code("emu_logits_constrain", good, c_set(layout=emu.Layout(MODEL, 2, 1, pad=64), stride=600), c, None) == "EMU_ERR_MISMATCH"
+    assert code("emu_logits_constrain", good, c_set(layout=emu.Layout(MODEL, 1, 1), stride=1000), c, None) == "EMU_ERR_MISMATCH"
+    # in place means the same set: not the same memory in another type or stride, nor half of it
+    assert code("emu_logits_constrain", good, c_set(dtype=emu.FP32), c, None) == "EMU_ERR_OVERLAP"
+    assert code("emu_logits_constrain", good, c_set(stride=512), c, None) == "EMU_ERR_OVERLAP"
+    assert code("emu_logits_constrain", good, c_set(shards=[ADDRESS, 2 * ADDRESS]), c, None) == "EMU_ERR_OVERLAP"
+    assert distill(good, c_teacher(), grad=ctypes.addressof(c_set(dtype=emu.FP32))) == "EMU_ERR_OVERLAP"
+    assert code("emu_logits_constrain", good, None, c, None) == "EMU_ERR_NULL"
+    assert code("emu_logits_constrain", good, good, None, None) == "EMU_ERR_NULL"
+
+
+@pytest.mark.parametrize("want,fields", [
+    ("EMU_ERR_NULL", dict(tokens=ADDRESS, tokens_cols=4, tokens_stride=4)),
+    ("EMU_ERR_ARG", dict(tokens=ADDRESS, tokens_cols=5, tokens_stride=4, seq_len=ADDRESS)),
+    ("EMU_ERR_ARG", dict(tokens=ADDRESS, tokens_cols=-1, tokens_stride=4, seq_len=ADDRESS)),
+    ("EMU_ERR_ALIGN", dict(tokens=ADDRESS + 2, tokens_cols=4, tokens_stride=4, seq_len=ADDRESS)),
+    ("EMU_ERR_ALIGN", dict(repetition=ADDRESS + 1)),
+    ("EMU_ERR_NULL", dict(bias_first=ADDRESS, n_bias=3, bias_token=ADDRESS)),
+    ("EMU_ERR_ARG", dict(bias_first=ADDRESS, n_bias=-1)),
+    ("EMU_ERR_ARG", dict(mask=ADDRESS, n_masks=4, mask_stride=31)),
+    ("EMU_ERR_ARG", dict(mask=ADDRESS, n_masks=3, mask_stride=32)),
+    ("EMU_ERR_ARG", dict(mask=ADDRESS, n_masks=-1, mask_stride=32, mask_row=ADDRESS)),
+])
+def test_constraints_are_checked(want, fields):
+    c = emu.c_constraints()
+    for k, v in fields.items():
+        setattr(c, k, v)
+    assert code("emu_logits_constrain", c_set(), c_set(), c, None) == want
+
+
+def test_topk_arguments():
+    l = c_set()
+    for k in (0, -1, 65):
+        assert topk(l, k=k) == "EMU_ERR_RANGE"
+    small = emu.Layout(emu.Model(2, 256, 8, 64, 8, 512, 32), 1, 1)
+    assert topk(c_set(layout=small, stride=32), k=33) == "EMU_ERR_RANGE"
+    for tau in (0.0, -1.0, float("nan"), float("inf"), 1e-38):
+        assert topk(l, tau=tau) == "EMU_ERR_ARG"
+    assert topk(l, index=None) == "EMU_ERR_NULL" and topk(l, logprob=None) == "EMU_ERR_NULL"
+    assert topk(l, lse=ADDRESS + 2) == "EMU_ERR_ALIGN"
+    n = ctypes.c_uint64()
+    assert code("emu_logits_workspace", l, 65, ctypes.addressof(n)) == "EMU_ERR_RANGE"
+    assert code("emu_logits_workspace", l, 4, None) == "EMU_ERR_NULL"
+
+
+@pytest.mark.parametrize("want,fields", [
+    ("EMU_ERR_RANGE", dict(k=0)), ("EMU_ERR_RANGE", dict(k=257, index_stride=257, value_stride=257)),
+    ("EMU_ERR_ARG", dict(tail=2)), ("EMU_ERR_ARG", dict(temperature=0.0)), ("EMU_ERR_ARG", dict(index_stride=7)),
+    ("EMU_ERR_ARG", dict(value_stride=7)), ("EMU_ERR_NULL", dict(index=None)), ("EMU_ERR_NULL", dict(value=None)),
+    ("EMU_ERR_ALIGN", dict(value=ADDRESS + 2)), ("EMU_ERR_ALIGN", dict(weight=ADDRESS + 2)),
+])
+def test_teachers_are_checked(want, fields):
+    l, te = c_set(), c_teacher(**fields)
+    assert distill(l, te) == want
+    assert code("emu_distill_backward", l, te, ADDRESS, l, ADDRESS, 1 << 40, None) == want
+
+
+def test_distill_operands():
+    l, te = c_set(), c_teacher()
+    assert distill(l, None) == "EMU_ERR_NULL"
+    assert distill(l, te, loss=None) == "EMU_ERR_NULL" and distill(l, te, stats=None) == "EMU_ERR_NULL"
+    assert distill(l, te, stats=ADDRESS + 4) == "EMU_ERR_ALIGN"
+    assert code("emu_distill_backward", l, te, None, l, ADDRESS, 1 << 40, None) == "EMU_ERR_NULL"
+    assert code("emu_distill_backward", l, te, ADDRESS, None, ADDRESS, 1 << 40, None) == "EMU_ERR_NULL"
+
+
+def test_no_rows_is_no_work():
+    l = c_set(rows=0, shards=[None, None])
+    assert topk(l, index=None, logprob=None, lse=None) == "EMU_OK"
+    te = c_teacher(index=None, value=None)
+    assert distill(l, te, loss=None, stats=None) == "EMU_OK"
+    assert code("emu_logits_constrain", l, l, emu.c_constraints(), None) == "EMU_OK"
+
+
+def test_workspace_does_not_depend_on_the_split():
+    big = emu.Model(2, 256, 8, 64, 8, 512, 128256)
+    sizes = set()
+    for tp, pad in ((1, 0), (2, 0), (4, 64), (8, 128)):
+        lay, n = emu.Layout(big, tp, 1, pad=pad), ctypes.c_uint64()
+        assert code("emu_logits_workspace", c_set(layout=lay, stride=1 << 18, rows=3), 20, ctypes.addressof(n)) == "EMU_OK"
+        sizes.add(n.value)
+    assert len(sizes) == 1
+
+
+def test_binding_refuses_before_the_library():
+    import torch
+
+    x = [torch.zeros(4, 500, dtype=torch.bfloat16) for _ in range(2)]
+    for bad in ([x[0]], [x[0], x[1][:, :499]], [x[0], x[1].float()], [x[0], x[1][:3]], [x[0].half(), x[1].half()],
+                [x[0], torch.zeros(4, 1000, dtype=torch.bfloat16)[:, ::2]], [x[0][0], x[1][0]]):
+        with pytest.raises(ValueError):
+            emu.LogitShards(LAY, bad)
+    with pytest.raises(ValueError, match="device"):
+        emu.LogitShards(LAY, x)
+    with pytest.raises(emu.EmuError):
+        emu.shard_columns(emu.Layout(MODEL, 3, 1))
+    assert [emu.shard_columns(emu.Layout(MODEL, tp, 1, pad=p)) for tp, p in ((1, 0), (4, 0), (8, 128), (2, 7))] == [1000, 250, 128, 504]
