@@ -387,7 +387,7 @@ int emu_check_bucket_tables(emu_plan_t plan, int32_t side, uint64_t bucket_bytes
  *     call must not overlap (undefined behaviour).
  *   - Sums, softmax statistics and losses are fp32 or wider, rounded to the output's type once. No result
  *     depends on the order of atomics.
- *   - Limits: tp <= 64, V <= 2^22, rows <= 2^31 - 1 (EMU_ERR_UNSUPPORTED); zero rows are a call that does nothing.
+ *   - Limits: tp <= 64, Vp <= 2^20, rows <= 2^31 - 1, 2^28 tokens per row (EMU_ERR_UNSUPPORTED); zero rows are a call that does nothing.
  *   - A workspace (emu_logits_workspace) holds what the workgroups of one call hand each other. It needs no
  *     initial contents and keeps nothing for later calls. Two calls that may run at the same time need two. */
 
@@ -466,7 +466,7 @@ int emu_logits_topk(const emu_logits_t* in, int32_t k, float temperature, int32_
  *           dL/dz_v = (q_v - p_v) / tau inside J, q_v (1 - p_R / q_R) / tau outside
  * Terms with p = 0 are 0. A column listed twice holds the sum of its entries' probabilities. With tail 0 a row
  * without an entry, or whose values are all -infinity, has L = 0 and gradient 0. Where p > 0 meets q = 0, L is
- * +infinity and the gradient keeps its finite part (q_R = 0: the factor outside J is 1); against q_R = 0 a p_R below
+ * +infinity and the gradient keeps its finite part (q_R < 2^-100: the factor outside J is 1); against q_R = 0 a p_R below
  * 2^-20, which the rounding of fp32 log-probabilities leaves, counts as 0.
  * d_loss[r] = w_r L_r. With grad (or NULL), its shards get w_r dL/dz, and 0 in every column from V on. d_stats
  * [rows][4], 16-byte aligned: lse of z/tau, the factor 1 - p_R/q_R (1 without a tail), the row's largest logit m and

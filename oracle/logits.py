@@ -104,7 +104,7 @@ def distill(z, index, value, weight=None, tau=1.0, tail=False):
                 q_rest = q[~listed].sum()
                 if rest > (0 if q_rest > 0 else 2.0 ** -20):
                     L += rest * (np.log(rest) - np.log(q_rest))
-                if q_rest != 0:
+                if not q_rest < 2.0 ** -100:
                     f = 1.0 - rest / q_rest
         loss[r], factor[r] = w * L, f
         grad[r] = w / tau * np.where(listed, q - p, q * f)

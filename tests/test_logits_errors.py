@@ -81,6 +81,7 @@ def test_outputs_must_be_the_inputs_kin():
     ("EMU_ERR_NULL", dict(tokens=ADDRESS, tokens_cols=4, tokens_stride=4)),
     ("EMU_ERR_ARG", dict(tokens=ADDRESS, tokens_cols=5, tokens_stride=4, seq_len=ADDRESS)),
     ("EMU_ERR_ARG", dict(tokens=ADDRESS, tokens_cols=-1, tokens_stride=4, seq_len=ADDRESS)),
+    ("EMU_ERR_UNSUPPORTED", dict(tokens=ADDRESS, tokens_cols=(1 << 28) + 1, tokens_stride=1 << 30, seq_len=ADDRESS)),
     ("EMU_ERR_ALIGN", dict(tokens=ADDRESS + 2, tokens_cols=4, tokens_stride=4, seq_len=ADDRESS)),
     ("EMU_ERR_ALIGN", dict(repetition=ADDRESS + 1)),
     ("EMU_ERR_NULL", dict(bias_first=ADDRESS, n_bias=3, bias_token=ADDRESS)),
