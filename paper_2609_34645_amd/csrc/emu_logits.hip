@@ -2,9 +2,11 @@
 // k largest log-probabilities, distillation with its gradient. Every row is read once (twice for a loss with its
 // gradient), in 16-byte vectors; every reduction runs over global columns in a fixed order, so that no result
 // depends on how the shards cut them.
+#include <algorithm>
 #include <cmath>
+#include <type_traits>
 
-#include "emu_internal.h"
+#include "emu_hip.h"
 
 namespace emu {
 
@@ -14,9 +16,8 @@ constexpr int32_t kMaxTokens = 1 << 28;  // of one row's history: byte offsets s
 constexpr int kMaxTop = 64;        // entries of emu_logits_topk: one per lane of a wave
 constexpr int kMaxTeacher = 256;   // entries of a teacher's row
 constexpr uint32_t kMaxSplits = 64;            // workgroups that share a row: one partial result per lane
-constexpr uint32_t kRowsPerLaunch = 1u << 21;  // a grid's work-items stay below 2^32
+constexpr uint32_t kRowsPerLaunch = 1u << 15;  // bounds a grid's work-items below 2^32, and the workspace that a call needs
 constexpr float kInf = __builtin_inff();
-constexpr float kLog2e = 1.44269504f;
 
 // A logits set on the device: row r's columns [t * cols, (t + 1) * cols) lie at p[t] + r * row_bytes.
 struct Logits {
@@ -35,10 +36,11 @@ __device__ __forceinline__ uint32_t shard_of(const Logits& l, uint32_t v) {
 // ------------------------------------------------------------------------------------------------
 // rows in vectors
 // ------------------------------------------------------------------------------------------------
-// A lane holds 16 bytes, kE<T> columns from a multiple of kE<T> on; a wave's tile is 64 such vectors, 1 KB, and a
-// wave takes U neighbouring tiles at a time. Columns are counted over the whole vocabulary, so which lane
-// adds up which column, and in which order, does not depend on the shards. Where the U tiles lie inside one
-// shard (all but one stretch per shard do), they are U loads from one scalar base at any element alignment;
+// A lane holds 16 bytes, kE<T> columns from a multiple of kE<T> on; a wave's tile is 64 such vectors, 1 KB. A workgroup
+// has a span of tiles and each of its waves a contiguous part of it, U tiles at a time: copies of rows ran at 6.3 TB/s
+// with 16 contiguous KB per wave, at 5.5 with the waves' 4 KB by turns. Columns are counted over the whole vocabulary, so
+// which lane adds up which column, and in which order, does not depend on the shards. Where the U tiles lie inside
+// one shard (all but one stretch per shard do), they are U loads from one scalar base at any element alignment;
 // elsewhere every lane finds its own shard, and a vector across a shard's end is put together by element.
 
 typedef uint16_t bf16_t;  // bits
@@ -73,6 +75,12 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){a, b}, b2));
 }
 
+template <typename T>
+__device__ __forceinline__ void set_minus_inf(v4u& x, uint32_t e) {
+  if constexpr (sizeof(T) == 2) x[e / 2] = e % 2 ? (x[e / 2] & 0xffffu) | 0xff800000u : (x[e / 2] & 0xffff0000u) | 0xff80u;
+  else x[e] = kMinusInf<T>;
+}
+
 // The vector of columns [v, v + kE) at a shard's or the vocabulary's end; -infinity from V on.
 template <typename T, int POL>
 __device__ v4u load_edge(const Logits& l, uint64_t row_off, uint32_t v) {
@@ -90,17 +98,81 @@ __device__ v4u load_edge(const Logits& l, uint64_t row_off, uint32_t v) {
   return x;
 }
 
-// The wave's U tiles from column c on (the same c in every lane).
+// Tiles [t0, t1) of a row.
+struct Span {
+  uint32_t t0, t1;
+};
+__device__ __forceinline__ Span part_of(Span s, uint32_t part, uint32_t parts) {
+  const uint32_t per = (s.t1 - s.t0 + parts - 1) / parts, t0 = umin(s.t0 + part * per, s.t1);
+  return {t0, umin(t0 + per, s.t1)};
+}
+__device__ __forceinline__ uint32_t wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+template <typename T> __host__ __device__ constexpr uint32_t tiles(uint32_t columns) { return (columns + kTile<T> - 1) / kTile<T>; }
+
+// Where a wave is in its row: column c, in shard t at column lo, at `base`. TILE: the tile's columns. Going on keeps
+// the shard's address; finding it anew (a load from the arguments) is for the few tiles that begin in another shard.
+template <typename T, uint32_t TILE>
+struct Cursor {
+  uint64_t row_off;
+  uint32_t c, t, lo;
+  uint8_t* base;
+  __device__ __forceinline__ Cursor(const Logits& l, uint64_t row_off, uint32_t tile) : row_off(row_off), c(tile * TILE), t(shard_of(l, c)), lo(c - t * l.cols) {
+    find(l);
+  }
+  __device__ __forceinline__ void find(const Logits& l) { base = l.p[umin(t, kMaxShards - 1)] + row_off + uint64_t(lo) * sizeof(T); }
+  __device__ __forceinline__ void advance(const Logits& l, uint32_t n) {
+    c += n * TILE;
+    lo += n * TILE;
+    base += n * TILE * sizeof(T);
+    if (lo >= l.cols) {
+      do {
+        lo -= l.cols;
+        ++t;
+      } while (lo >= l.cols);
+      find(l);
+    }
+  }
+  // n tiles wholly in one shard and below V
+  __device__ __forceinline__ bool one(const Logits& l, uint32_t n) const { return lo + n * TILE <= l.cols && c + n * TILE <= l.V; }
+  // the base as seen from the next shard
+  __device__ __forceinline__ uint8_t* other(const Logits& l) const { return l.p[umin(t + 1, kMaxShards - 1)] + row_off - uint64_t(l.cols - lo) * sizeof(T); }
+};
+template <typename T> using Reader = Cursor<T, kTile<T>>;
+
+// A tile that is not wholly in one shard and below V. Where shards are no shorter than a tile it lies in two at
+// most, and only a vector across their border goes by element (WHOLE: there is none).
+template <typename T, int POL, bool WHOLE = false>
+__device__ __forceinline__ v4u load_border(const Logits& l, const Reader<T>& at, uint32_t lane) {
+  const uint32_t v = at.c + lane * kE<T>, lo = at.lo + lane * kE<T>;
+  if (!WHOLE && (l.cols < kTile<T> || (lo < l.cols && lo + kE<T> > l.cols))) return load_edge<T, POL>(l, at.row_off, v);
+  v4u x = {kMinusInf<T>, kMinusInf<T>, kMinusInf<T>, kMinusInf<T>};
+  if (v >= l.V) return x;
+  x = ld16_any<POL>(lo >= l.cols ? at.other(l) : at.base, lane * 16);
+  if (v + kE<T> > l.V) {  // pads behind V in V's own vector
+#pragma unroll
+    for (uint32_t e = 0; e < kE<T>; ++e)
+      if (v + e >= l.V) set_minus_inf<T>(x, e);
+  }
+  return x;
+}
+
+// U tiles from the cursor on, which goes behind them; -infinity from tile `end` on.
 template <typename T, int U, int POL>
-__device__ __forceinline__ void load_tiles(const Logits& l, uint64_t row_off, uint32_t c, v4u (&x)[U]) {
-  const uint32_t lane = threadIdx.x & 63, t = shard_of(l, c), lo = c - t * l.cols;
-  if (lo + U * kTile<T> <= l.cols && c + U * kTile<T> <= l.V) {
-    const uint8_t* base = l.p[t] + row_off + uint64_t(lo) * sizeof(T);
+__device__ __forceinline__ void load_tiles(const Logits& l, Reader<T>& at, uint32_t end, v4u (&x)[U]) {
+  const uint32_t lane = threadIdx.x & 63;
+  if (at.one(l, U) && at.c + U * kTile<T> <= end * kTile<T>) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = ld16_any<POL>(base, lane * 16 + u * 1024);
-  } else {
+    for (int u = 0; u < U; ++u) x[u] = ld16_any<POL>(at.base, lane * 16 + u * 1024);
+    at.advance(l, U);
+    return;
+  }
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = load_edge<T, POL>(l, row_off, c + u * kTile<T> + lane * kE<T>);
+  for (int u = 0; u < U; ++u) {
+    x[u] = (v4u){kMinusInf<T>, kMinusInf<T>, kMinusInf<T>, kMinusInf<T>};
+    if (at.c >= end * kTile<T>) continue;
+    if (at.one(l, 1)) x[u] = ld16_any<POL>(at.base, lane * 16);
+    else x[u] = load_border<T, POL>(l, at, lane);
+    at.advance(l, 1);
   }
 }
 
@@ -136,15 +208,53 @@ __device__ void store_edge(const Logits& l, uint64_t row_off, uint32_t v, const 
   }
 }
 
+// The tile at `at`, N columns a lane. WHOLE: no vector crosses a shard's end.
+template <typename TO, int POL, uint32_t N, bool WHOLE = false>
+__device__ __forceinline__ void store_tile(const Logits& l, const Cursor<TO, 64 * N>& at, uint32_t lane, const float (&f)[N]) {
+  uint8_t* base = at.base;
+  if (!at.one(l, 1)) {
+    const uint32_t lo = at.lo + lane * N;
+    if (!WHOLE && (l.cols < 64 * N || (lo < l.cols && lo + N > l.cols))) return store_edge<TO, POL, N>(l, at.row_off, at.c + lane * N, f);
+    if (at.c + lane * N >= l.Vp) return;
+    if (lo >= l.cols) base = at.other(l);
+  }
+  store_values<TO, POL>(base, lane * N * uint32_t(sizeof(TO)), f);
+}
+
 // ------------------------------------------------------------------------------------------------
 // reductions in fixed trees
 // ------------------------------------------------------------------------------------------------
 
+// x of the lane whose number differs in bit N, in vector instructions (a shuffle through LDS takes a trip to it).
+template <int N>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
+  if constexpr (N == 1) return __builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true);   // quad_perm 1 0 3 2
+  if constexpr (N == 2) return __builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true);   // quad_perm 2 3 0 1
+  if constexpr (N == 4) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true), 0x1b, 0xf, 0xf, true);  // 7 - i, then 3 - i
+  if constexpr (N == 8) return __builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, true);  // row_ror 8
+  if constexpr (N == 16) {
+    const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return threadIdx.x & 16 ? y[0] : y[1];
+  }
+  if constexpr (N == 32) {
+    const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return threadIdx.x & 32 ? y[0] : y[1];
+  }
+}
+template <int N> __device__ __forceinline__ float lane_xor(float x) { return __uint_as_float(lane_xor<N>(__float_as_uint(x))); }
+template <int N> __device__ __forceinline__ uint64_t lane_xor(uint64_t x) {
+  return uint64_t(lane_xor<N>(uint32_t(x >> 32))) << 32 | lane_xor<N>(uint32_t(x));
+}
+template <int N> __device__ __forceinline__ double lane_xor(double x) { return __longlong_as_double(lane_xor<N>(uint64_t(__double_as_longlong(x)))); }
+
 template <typename T, typename F>
 __device__ __forceinline__ T wave_reduce(T x, F f) {
-#pragma unroll
-  for (int n = 32; n; n >>= 1) x = f(x, __shfl_xor(x, n));
-  return x;
+  x = f(x, lane_xor<32>(x));
+  x = f(x, lane_xor<16>(x));
+  x = f(x, lane_xor<8>(x));
+  x = f(x, lane_xor<4>(x));
+  x = f(x, lane_xor<2>(x));
+  return f(x, lane_xor<1>(x));
 }
 
 // Over the workgroup's NW waves; every thread gets the result. Two barriers.
@@ -186,31 +296,34 @@ struct Running {
 __device__ __forceinline__ float reference(float m, float c1) { return fmaxf(m * c1, -kPlainRange); }
 __device__ __forceinline__ bool plain(float m, float c1) { return fabsf(m * c1) < kPlainRange; }
 
-__device__ __forceinline__ Running joined(Running a, Running b, float c1) {
-  const float m = fmaxf(a.m, b.m), ref = reference(m, c1);
-  const float ea = __builtin_amdgcn_exp2f(reference(a.m, c1) - ref), eb = __builtin_amdgcn_exp2f(reference(b.m, c1) - ref);
-  return {m, a.s * ea + b.s * eb};
+// n statistics to one: relative to the largest maximum, summed in order.
+template <int N>
+__device__ __forceinline__ Running joined(const Running (&a)[N], float c1) {
+  Running j = a[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) j.m = fmaxf(j.m, a[i].m);
+  const float ref = reference(j.m, c1);
+  j.s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) j.s += a[i].s * __builtin_amdgcn_exp2f(reference(a[i].m, c1) - ref);
+  return j;
 }
 
 __device__ __forceinline__ Running wave_joined(Running a, float c1) {
-#pragma unroll
-  for (int n = 32; n; n >>= 1) {
-    const Running b = {__shfl_xor(a.m, n), __shfl_xor(a.s, n)};
-    a = joined(a, b, c1);
-  }
-  return a;
+  const float m = wave_reduce(a.m, [](float x, float y) { return fmaxf(x, y); });
+  return {m, wave_reduce(a.s * __builtin_amdgcn_exp2f(reference(a.m, c1) - reference(m, c1)), add)};
 }
 
+// Over the workgroup, in every thread. lds must not be in use: the caller has passed a barrier since it was.
 template <int NW>
 __device__ __forceinline__ Running block_joined(Running a, Running* lds, float c1) {
   a = wave_joined(a, c1);
-  __syncthreads();
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
   __syncthreads();
-  a = lds[0];
+  Running all[NW];
 #pragma unroll
-  for (int w = 1; w < NW; ++w) a = joined(a, lds[w], c1);
-  return a;
+  for (int w = 0; w < NW; ++w) all[w] = lds[w];
+  return joined(all, c1);
 }
 
 // U vectors of a lane.
@@ -236,8 +349,6 @@ __device__ __forceinline__ float true_sum(Running r, float c1) {
   return r.s * __builtin_amdgcn_exp2f(-fmaf(r.m, c1, -reference(r.m, c1)));
 }
 
-__device__ __forceinline__ uint32_t wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-
 // Sum of exp((x - m) / tau) over the row by the whole workgroup; marked columns (a bit each from column 0 on) are
 // left out.
 template <typename T, int NW>
@@ -260,15 +371,6 @@ __device__ __forceinline__ float log_sum_exp(float m, float s, float c1) {
 // log(exp((x - m) / tau) / s), likewise.
 __device__ __forceinline__ float log_prob(float x, float m, float s, float c1) {
   return x == -kInf ? -kInf : float(((double(x) - double(m)) * double(c1) - double(log2f(s))) * 0.6931471805599453);
-}
-
-// The columns of workgroup `part` of the `parts` that share a row, in whole chunks of U tiles per wave.
-template <typename T, int U, int NW>
-__device__ __forceinline__ void part_range(uint32_t end, uint32_t part, uint32_t parts, uint32_t* c0, uint32_t* c1) {
-  constexpr uint32_t kChunk = U * kTile<T>;
-  const uint32_t chunks = (end + kChunk - 1) / kChunk, per = (chunks + parts - 1) / parts;
-  *c0 = umin(part * per, chunks) * kChunk;
-  *c1 = umin(*c0 + per * kChunk, end);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -452,27 +554,23 @@ __device__ __forceinline__ uint64_t lane_key(uint64_t x, uint32_t lane) {  // th
   return uint64_t(__builtin_amdgcn_readlane(uint32_t(x >> 32), lane)) << 32 | uint32_t(__builtin_amdgcn_readlane(uint32_t(x), lane));
 }
 
-__device__ __forceinline__ uint64_t sorted(uint64_t x) {  // across the wave, largest in lane 0
+template <uint32_t K, uint32_t J>
+__device__ __forceinline__ uint64_t sort_step(uint64_t x) {  // larger ones to the lanes without bit J, in blocks of K by turns
   const uint32_t lane = threadIdx.x & 63;
-#pragma unroll
-  for (uint32_t k = 2; k <= 64; k <<= 1) {
-#pragma unroll
-    for (uint32_t j = k >> 1; j; j >>= 1) {
-      const uint64_t y = __shfl_xor((unsigned long long)x, j);
-      x = ((lane & j) == 0) == ((lane & k) == 0) ? max64(x, y) : min64(x, y);
-    }
-  }
+  const uint64_t y = lane_xor<J>(x);
+  return ((lane & J) == 0) == ((lane & K) == 0) ? max64(x, y) : min64(x, y);
+}
+template <uint32_t K, uint32_t J = K / 2>
+__device__ __forceinline__ uint64_t sort_steps(uint64_t x) {
+  x = sort_step<K, J>(x);
+  if constexpr (J > 1) return sort_steps<K, J / 2>(x);
   return x;
 }
+__device__ __forceinline__ uint64_t sorted(uint64_t x) {  // across the wave, largest in lane 0
+  return sort_steps<64>(sort_steps<32>(sort_steps<16>(sort_steps<8>(sort_steps<4>(sort_steps<2>(x))))));
+}
 __device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b) {  // the 64 largest of two sorted waves, sorted
-  const uint32_t lane = threadIdx.x & 63;
-  uint64_t x = max64(a, __shfl((unsigned long long)b, 63 - lane));
-#pragma unroll
-  for (uint32_t j = 32; j; j >>= 1) {
-    const uint64_t y = __shfl_xor((unsigned long long)x, j);
-    x = (lane & j) == 0 ? max64(x, y) : min64(x, y);
-  }
-  return x;
+  return sort_steps<64>(max64(a, __shfl((unsigned long long)b, 63 - (threadIdx.x & 63))));
 }
 
 // What the wave's lanes wrote to LDS is what its lanes read from here on.
@@ -528,12 +626,11 @@ template <typename T>
 __global__ __launch_bounds__(kTopWaves * 64) void k_topk(Logits in, uint32_t k, float c1, int32_t* index, float* logprob,
                                                          float* lse, Running* part_run, uint64_t* part_keys, uint64_t row0) {
   constexpr int NW = kTopWaves, U = kTopU;
-  constexpr uint32_t E = kE<T>, kChunk = U * kTile<T>;
+  constexpr uint32_t E = kE<T>;
   __shared__ TopLds<NW> t;
   const uint64_t r = row0 + blockIdx.x, off = r * in.row_bytes;
   const uint32_t lane = threadIdx.x & 63, w = wave_id();
-  uint32_t c0, end;
-  part_range<T, U, NW>(in.V, blockIdx.y, gridDim.y, &c0, &end);
+  const Span span = part_of(part_of({0, tiles<T>(in.V)}, blockIdx.y, gridDim.y), w, NW);
   if (threadIdx.x == 0) t.bound = 0;
   __syncthreads();
   uint64_t best = 0, bound = 0;  // every key in the row's result is >= bound
@@ -548,9 +645,11 @@ __global__ __launch_bounds__(kTopWaves * 64) void k_topk(Logits in, uint32_t k, 
   };
   Running run = {-kInf, 0.0f};
   bool first = true;
-  for (uint32_t c = c0 + w * kChunk; c < end; c += NW * kChunk) {
+  Reader<T> at(in, off, span.t0);
+  for (uint32_t tile = span.t0; tile < span.t1; tile += U) {
+    const uint32_t c = tile * kTile<T>;
     v4u x[U];
-    load_tiles<T, U, POL_NT>(in, off, c, x);
+    load_tiles<T, U, POL_NT>(in, at, span.t1, x);
     float f[U][E], top[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -628,8 +727,8 @@ __global__ __launch_bounds__(kTopWaves * 64) void k_topk_join(Logits in, uint32_
 // again, from cache. Where they are few, several share a row: they scan a part each and leave its statistics in
 // the workspace, a second kernel joins them to the row's, and the gradient goes by parts again (in place, no part
 // may be written before every reader of the row is done: hence the kernel between).
-// The gradient is written densely as coef * exp((z - m) / tau), and the listed columns, whose values the
-// threads have kept, are written over it behind a barrier. With a tail the scan leaves out the listed
+// The gradient is coef * exp((z - m) / tau), but for the listed columns, whose gradients come from their entries'
+// threads by way of LDS. With a tail the scan leaves out the listed
 // columns (a bit each in LDS), so that a small mass outside the list is a sum of its own and no difference.
 
 // A list of log-probabilities rounded to fp32 can miss a sum of 1 by sum p |log p| 2^-24 < 2^-20.
@@ -652,21 +751,28 @@ struct DistillLds {
   Running run[NW];
 };
 
-// Logits are read in columns [z0, z1). rest: the mass outside the list (0 without a tail); none: without a tail nothing is listed.
+// Entry j of row r as it is stored.
+struct Stored {
+  int32_t col;
+  float value;
+};
+__device__ __forceinline__ Stored fetch_teacher(const emu_teacher_t& te, uint64_t r, uint32_t V) {
+  const int j = threadIdx.x;
+  if (j >= te.k) return {-1, 0.0f};
+  const Stored f = {te.index[r * te.index_stride + j], te.value[r * te.value_stride + j]};
+  return {uint32_t(f.col) < V ? f.col : -1, f.value};
+}
+
+// Logits are read in columns [z0, z1). rest: the mass outside the list (0 without a tail); none: without a tail
+// nothing is listed.
 template <typename T, int NW>
-__device__ __forceinline__ Entry load_teacher(DistillLds<NW>& t, const emu_teacher_t& te, uint64_t r, const Logits& l, uint32_t z0, uint32_t z1, float* rest, bool* none) {
+__device__ __forceinline__ Entry take_teacher(DistillLds<NW>& t, Stored f, const emu_teacher_t& te, uint64_t r, const Logits& l, uint32_t z0,
+                                              uint32_t z1, float* rest, bool* none) {
   static_assert(NW * 64 >= kMaxTeacher, "one entry per thread");
   const int j = threadIdx.x;
-  Entry e = {-1, 0.0f, -kInf};
-  double value = -double(kInf);
-  if (j < te.k) {
-    const int32_t i = te.index[r * te.index_stride + j];
-    if (uint32_t(i) < l.V) {
-      e.col = i;
-      if (uint32_t(i) >= z0 && uint32_t(i) < z1) e.z = widen(*column<T>(l, r * l.row_bytes, i));
-      value = double(te.value[r * te.value_stride + j]);
-    }
-  }
+  Entry e = {f.col, 0.0f, -kInf};
+  if (e.col >= 0 && uint32_t(e.col) >= z0 && uint32_t(e.col) < z1) e.z = widen(*column<T>(l, r * l.row_bytes, e.col));
+  const double value = e.col >= 0 ? double(f.value) : -double(kInf);
   double top = 0.0;
   if (!te.tail) {
     top = block_reduce<NW>(value, t.wide, [](double a, double b) { return fmax(a, b); });
@@ -680,7 +786,7 @@ __device__ __forceinline__ Entry load_teacher(DistillLds<NW>& t, const emu_teach
     t.p[j] = p;
   }
   __syncthreads();
-  if (j < te.k && e.col >= 0) {
+  if (e.col >= 0) {
     bool first = true;
     for (int i = 0; i < te.k; ++i) {
       if (i == j || t.col[i] != e.col) continue;
@@ -698,40 +804,51 @@ __device__ __forceinline__ Entry load_teacher(DistillLds<NW>& t, const emu_teach
 
 // A bit per listed column of [c0, c0 + range), range a multiple of 32.
 template <int NW>
-__device__ __forceinline__ void mark_listed(uint32_t* bits, uint32_t c0, uint32_t range, const emu_teacher_t& te, uint64_t r, uint32_t V) {
+__device__ __forceinline__ void mark_listed(uint32_t* bits, uint32_t c0, uint32_t range, int32_t col) {
   for (uint32_t i = threadIdx.x; i < range / 32; i += NW * 64) bits[i] = 0;
   __syncthreads();
-  if (int(threadIdx.x) < te.k) {
-    const uint32_t v = uint32_t(te.index[r * te.index_stride + threadIdx.x]), at = v - c0;
-    if (v < V && at < range) atomicOr(&bits[at / 32], 1u << (at % 32));
-  }
+  const uint32_t at = uint32_t(col) - c0;
+  if (col >= 0 && at < range) atomicOr(&bits[at / 32], 1u << (at % 32));
   __syncthreads();
 }
 
-// The statistics of columns [c0, end), without the marked ones if TAIL.
-template <typename T, int U, int NW, bool TAIL, int POL>
-__device__ __forceinline__ Running scan(const Logits& l, uint64_t off, uint32_t c0, uint32_t end, float c1, const uint32_t* bits) {
-  constexpr uint32_t E = kE<T>, kChunk = U * kTile<T>;
+// -infinity in the vector's marked columns; `at` counts from the first marked column on.
+template <typename T>
+__device__ __forceinline__ void leave_out(v4u& x, const uint32_t* bits, uint32_t at) {
+  const uint32_t hit = (reinterpret_cast<const uint8_t*>(bits)[at / 8] >> (at % 8)) & ((1u << kE<T>) - 1);
+  if (hit) {
+#pragma unroll
+    for (uint32_t e = 0; e < kE<T>; ++e)
+      if ((hit >> e) & 1u) set_minus_inf<T>(x, e);
+  }
+}
+
+// The wave's statistics of its part of the workgroup's span, without the marked columns if TAIL. The next tiles
+// are on their way while these are added up.
+constexpr int kScanU = 2;
+template <typename T, int NW, bool TAIL, int POL>
+__device__ __forceinline__ Running scan(const Logits& l, uint64_t off, Span block, float c1, const uint32_t* bits) {
+  constexpr int U = kScanU;
+  constexpr uint32_t E = kE<T>;
   const uint32_t lane = threadIdx.x & 63;
+  const Span span = part_of(block, wave_id(), NW);
   Running run = {-kInf, 0.0f};
-  for (uint32_t c = c0 + wave_id() * kChunk; c < end; c += NW * kChunk) {
-    v4u x[U];
-    load_tiles<T, U, POL>(l, off, c, x);
+  v4u x[U];
+  Reader<T> at(l, off, span.t0);
+  if (span.t0 < span.t1) load_tiles<T, U, POL>(l, at, span.t1, x);
+  for (uint32_t t = span.t0; t < span.t1; t += U) {
+    v4u y[U];
+    if (t + U < span.t1) load_tiles<T, U, POL>(l, at, span.t1, y);
     float f[U][E];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if constexpr (TAIL)
+        if (t + u < span.t1) leave_out<T>(x[u], bits, (t + u - block.t0) * kTile<T> + lane * E);
       unpack(x[u], f[u]);
-      if constexpr (TAIL) {
-        const uint32_t at = c - c0 + u * kTile<T> + lane * E;
-        const uint32_t hit = (reinterpret_cast<const uint8_t*>(bits)[at / 8] >> (at % 8)) & ((1u << E) - 1);
-        if (hit) {
-#pragma unroll
-          for (uint32_t e = 0; e < E; ++e)
-            if ((hit >> e) & 1u) f[u][e] = -kInf;
-        }
-      }
     }
     add_values<U, E>(run, f, c1);
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = y[u];
   }
   return run;
 }
@@ -740,53 +857,122 @@ struct Stats {
   float lse, factor, m, s;
 };
 
-// From the scan of a whole row: its statistics and loss, in every thread.
+// An entry as a part of the softmax's statistics.
+__device__ __forceinline__ Running entry_run(const Entry& e, float c1) {
+  if (e.col < 0) return {-kInf, 0.0f};
+  const float m = fmaxf(e.z, -kInf);
+  return {m, __builtin_amdgcn_exp2f(fmaf(e.z, c1, -reference(m, c1)))};
+}
+
+// A row's statistics from the scan's (with a tail: of the columns outside the list) and the entries', and the rest's
+// share of the loss. In every thread alike.
 template <typename T, int NW, bool TAIL>
-__device__ __forceinline__ Stats finish(const Logits& l, uint64_t off, Running run, const Entry& e, float rest, int k, float c1,
-                                        DistillLds<NW>& t, float* loss) {
-  Stats st;
-  float s = plain(run.m, c1) ? true_sum(run, c1)
-            : run.m == -kInf ? run.s
-                             : careful_sum<T, NW>(l, off, run.m, c1, t.col, TAIL ? k : 0, t.sum);
-  st.factor = 1.0f;
-  float rest_loss = 0.0f;
-  st.m = run.m;
-  st.s = s;
+__device__ __forceinline__ Stats conclude(const Logits& l, uint64_t off, Running run, Running inside, const Entry& e, float rest, int k,
+                                          float c1, DistillLds<NW>& t, float* rest_loss) {
+  const float s = plain(run.m, c1) ? true_sum(run, c1)
+                  : run.m == -kInf ? run.s
+                                   : careful_sum<T, NW>(l, off, run.m, c1, t.col, TAIL ? k : 0, t.sum);
+  Stats st = {0.0f, 1.0f, run.m, s};
+  *rest_loss = 0.0f;
   if constexpr (TAIL) {
-    const float z = e.col >= 0 ? e.z : -kInf;
-    st.m = fmaxf(run.m, block_reduce<NW>(z, t.sum, [](float a, float b) { return fmaxf(a, b); }));
+    float s_in = inside.s;
+    if (plain(inside.m, c1)) s_in = true_sum(inside, c1);
+    else if (inside.m != -kInf) s_in = block_reduce<NW>(e.col >= 0 ? __builtin_amdgcn_exp2f((e.z - inside.m) * c1) : 0.0f, t.sum, add);
+    st.m = fmaxf(run.m, inside.m);
     const float m = st.m == -kInf ? 0.0f : st.m;
-    const float inside = block_reduce<NW>(e.col >= 0 ? __builtin_amdgcn_exp2f((z - m) * c1) : 0.0f, t.sum, add);
-    st.s = (s == 0.0f ? 0.0f : s * __builtin_amdgcn_exp2f((run.m - m) * c1)) + inside;
+    st.s = (s == 0.0f ? 0.0f : s * __builtin_amdgcn_exp2f((run.m - m) * c1)) + (s_in == 0.0f ? 0.0f : s_in * __builtin_amdgcn_exp2f((inside.m - m) * c1));
     const float log_q = s == 0.0f ? -kInf
                                   : float(((double(run.m) - double(st.m)) * double(c1) + double(log2f(s)) - double(log2f(st.s))) * 0.6931471805599453);
-    if (rest != 0.0f && (s != 0.0f || rest >= kRestNoise)) rest_loss = rest * (logf(rest) - log_q);
+    if (rest != 0.0f && (s != 0.0f || rest >= kRestNoise)) *rest_loss = rest * (logf(rest) - log_q);
     const float q = expf(log_q);
     if (!(q < kLeastRest)) st.factor = 1.0f - rest / q;
   }
   st.lse = log_sum_exp(st.m, st.s, c1);
-  const float part = e.p != 0.0f ? e.p * (logf(e.p) - log_prob(e.z, st.m, st.s, c1)) : 0.0f;
-  *loss = block_reduce<NW>(part, t.sum, add) + rest_loss;
   return st;
 }
 
-// Dense: coef * exp((z - m) / tau) over columns [c0, end) of the padded row, 0 behind V. ZERO: 0, and nothing is read.
+__device__ __forceinline__ float entry_loss(const Entry& e, Stats st, float c1) {
+  return e.p != 0.0f ? e.p * (logf(e.p) - log_prob(e.z, st.m, st.s, c1)) : 0.0f;
+}
+
+// conclude with the loss, in every thread.
+template <typename T, int NW, bool TAIL>
+__device__ __forceinline__ Stats finish(const Logits& l, uint64_t off, Running run, const Entry& e, float rest, int k, float c1,
+                                        DistillLds<NW>& t, float* loss) {
+  Running inside = {-kInf, 0.0f};
+  __syncthreads();
+  if constexpr (TAIL) inside = block_joined<NW>(entry_run(e, c1), t.run, c1);
+  float rest_loss;
+  const Stats st = conclude<T, NW, TAIL>(l, off, run, inside, e, rest, k, c1, t, &rest_loss);
+  *loss = block_reduce<NW>(entry_loss(e, st, c1), t.sum, add) + rest_loss;
+  return st;
+}
+
+// The listed columns' gradients in LDS, chained by tile, for the lanes that hold the columns: writing them behind the
+// dense gradient instead, two bytes here and there, cost 24 of 398 us (4,096 rows of 128,256, 64 entries).
+template <int TILES>
+struct Listed {
+  int16_t head[TILES], next[kMaxTeacher];  // -1: none
+  int32_t col[kMaxTeacher];
+  float d[kMaxTeacher];
+};
+
+__device__ __forceinline__ float entry_gradient(const Entry& e, Stats st, float c1, float scale) {
+  const float q = st.s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((e.z - st.m) * c1) / st.s;
+  return (q - e.p) * scale;
+}
+
+// Entry j (thread j) into its tile's chain. The heads are -1 and a barrier has been passed; another must follow. The
+// order within a chain is any: its columns differ.
+template <typename T, int TILES>
+__device__ __forceinline__ void chain(Listed<TILES>& list, uint32_t t0, const Entry& e, float d) {
+  if (e.col < 0) return;
+  const uint32_t at = uint32_t(e.col) / kTile<T> - t0;
+  // heads are halves of words: exchange the half by comparison
+  uint32_t* word = reinterpret_cast<uint32_t*>(list.head) + at / 2;
+  const uint32_t shift = at % 2 * 16;
+  uint32_t old = *word, want;
+  do {
+    want = old;
+    old = atomicCAS(word, want, (want & ~(0xffffu << shift)) | uint32_t(threadIdx.x) << shift);
+  } while (old != want);
+  list.next[threadIdx.x] = int16_t(old >> shift);
+  list.col[threadIdx.x] = e.col;
+  list.d[threadIdx.x] = d;
+}
+
+// The tile's listed columns in place of the dense values; head the same in every lane.
+template <int TILES, uint32_t E>
+__device__ __forceinline__ void take_listed(const Listed<TILES>& list, int head, uint32_t v, float (&f)[E]) {
+  while (head >= 0) {
+    const uint32_t at = uint32_t(list.col[head]) - v;
+    const float d = list.d[head];
+#pragma unroll
+    for (uint32_t e = 0; e < E; ++e) f[e] = at == e ? d : f[e];
+    head = __builtin_amdgcn_readfirstlane(list.next[head]);
+  }
+}
+
+// Dense: coef * exp((z - m) / tau) over the workgroup's span of the padded row, 0 behind V, the listed columns'
+// values in their places. ZERO: 0 for the dense part, and no logits are read.
 enum Dense { PLAIN_RANGE, ANY_RANGE, ZERO };
-template <typename TI, typename TO, int U, int NW, int POL, Dense KIND>
-__device__ __forceinline__ void dense_gradient(const Logits& in, const Logits& out, uint64_t r, uint32_t c0, uint32_t end, float m,
+template <typename TI, typename TO, int U, int NW, int POL, Dense KIND, int TILES>
+__device__ __forceinline__ void dense_gradient(const Logits& in, const Logits& out, uint64_t r, Span block, const Listed<TILES>* list, float m,
                                                float c1, float coef) {
-  constexpr uint32_t E = kE<TI>, kChunk = U * kTile<TI>;
+  constexpr uint32_t E = kE<TI>;
   const uint32_t lane = threadIdx.x & 63;
   const uint64_t ri = r * in.row_bytes, ro = r * out.row_bytes;
   const float ref = reference(m, c1);
-  for (uint32_t c = c0 + wave_id() * kChunk; c < end; c += NW * kChunk) {
+  const Span span = part_of(block, wave_id(), NW);
+  const int heads = list && span.t0 + lane < span.t1 ? list->head[span.t0 + lane - block.t0] : -1;  // a wave has at most 64 tiles
+  Reader<TI> from(in, ri, span.t0);
+  Cursor<TO, kTile<TI>> to(out, ro, span.t0);
+  for (uint32_t tile = span.t0; tile < span.t1; tile += U) {
     v4u x[U];
-    if constexpr (KIND != ZERO) load_tiles<TI, U, POL>(in, ri, c, x);
-    const uint32_t t = shard_of(out, c), lo = c - t * out.cols;
-    const bool inside = lo + kChunk <= out.cols && c + kChunk <= out.V;
-    uint8_t* base = out.p[t] + ro + uint64_t(lo) * sizeof(TO);
+    if constexpr (KIND != ZERO) load_tiles<TI, U, POL>(in, from, span.t1, x);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if (tile + u >= span.t1) break;
       float f[E];
       if constexpr (KIND != ZERO) unpack(x[u], f);
 #pragma unroll
@@ -794,48 +980,35 @@ __device__ __forceinline__ void dense_gradient(const Logits& in, const Logits& o
         if constexpr (KIND == ZERO) f[e] = 0.0f;
         else f[e] = __builtin_amdgcn_exp2f(KIND == PLAIN_RANGE ? fmaf(f[e], c1, -ref) : (f[e] - m) * c1) * coef;
       }
-      const uint32_t v = c + u * kTile<TI> + lane * E;
-      if (inside) {
-        store_values<TO, POL_NT>(base, (u * kTile<TI> + lane * E) * uint32_t(sizeof(TO)), f);
-      } else if (v < end) {
+      const uint32_t v = to.c + lane * E;
+      if (to.c + kTile<TI> > in.V) {
 #pragma unroll
         for (uint32_t e = 0; e < E; ++e)
           if (v + e >= in.V) f[e] = 0.0f;
-        store_edge<TO, POL_NT>(out, ro, v, f);
       }
+      if (list) take_listed(*list, __builtin_amdgcn_readlane(heads, tile + u - span.t0), v, f);
+      store_tile<TO, POL_NT>(out, to, lane, f);
+      to.advance(out, 1);
     }
   }
 }
 
-// The listed columns of [c0, end), behind the dense gradient.
-template <typename TO>
-__device__ __forceinline__ void listed_gradient(const Logits& out, uint64_t r, uint32_t c0, uint32_t end, const Entry& e, Stats st,
-                                                float c1, float scale) {
-  __syncthreads();
-  if (e.col >= 0 && uint32_t(e.col) >= c0 && uint32_t(e.col) < end) {
-    const float q = st.s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((e.z - st.m) * c1) / st.s;
-    const float d = (q - e.p) * scale;
-    TO* at = const_cast<TO*>(column<TO>(out, r * out.row_bytes, e.col));
-    if constexpr (sizeof(TO) == 2) *at = bf16_t(pack2(d, d));
-    else *at = d;
-  }
-}
-
-// Row r's gradient over [c0, end), from its statistics.
-template <typename TI, typename TO, int U, int NW, int POL>
-__device__ __forceinline__ void row_gradient(const Logits& in, const Logits& out, uint64_t r, uint32_t c0, uint32_t end, const Entry& e,
+// Row r's gradient over the span, from its statistics. The heads of the list are -1, behind a barrier.
+template <typename TI, typename TO, int U, int NW, int POL, int TILES>
+__device__ __forceinline__ void row_gradient(const Logits& in, const Logits& out, uint64_t r, Span block, Listed<TILES>& list, const Entry& e,
                                              Stats st, float c1, float w, bool none) {
   const float scale = w * (c1 * 0.69314718f);  // w / tau
-  const bool dead = w == 0.0f || none;
-  if (dead || st.s == 0.0f) {
-    dense_gradient<TI, TO, U, NW, POL, ZERO>(in, out, r, c0, end, st.m, c1, 0.0f);
+  if (w == 0.0f || none) return dense_gradient<TI, TO, U, NW, POL, ZERO, TILES>(in, out, r, block, nullptr, st.m, c1, 0.0f);
+  chain<TI>(list, block.t0, e, entry_gradient(e, st, c1, scale));
+  __syncthreads();
+  if (st.s == 0.0f) {
+    dense_gradient<TI, TO, U, NW, POL, ZERO>(in, out, r, block, &list, st.m, c1, 0.0f);
   } else if (plain(st.m, c1)) {
     const float one = __builtin_amdgcn_exp2f(-fmaf(st.m, c1, -reference(st.m, c1)));  // exp2(ref - m * c1)
-    dense_gradient<TI, TO, U, NW, POL, PLAIN_RANGE>(in, out, r, c0, end, st.m, c1, scale * st.factor * (one / st.s));
+    dense_gradient<TI, TO, U, NW, POL, PLAIN_RANGE>(in, out, r, block, &list, st.m, c1, scale * st.factor * (one / st.s));
   } else {
-    dense_gradient<TI, TO, 1, NW, POL, ANY_RANGE>(in, out, r, c0, end, st.m, c1, scale * st.factor / st.s);
+    dense_gradient<TI, TO, 1, NW, POL, ANY_RANGE>(in, out, r, block, &list, st.m, c1, scale * st.factor * (1.0f / st.s));
   }
-  if (!dead) listed_gradient<TO>(out, r, c0, end, e, st, c1, scale);
 }
 
 __device__ __forceinline__ void write_row(float* loss, float4* stats, uint64_t r, float value, Stats st) {
@@ -846,29 +1019,258 @@ __device__ __forceinline__ void write_row(float* loss, float4* stats, uint64_t r
 }
 constexpr Stats kSkipped = {__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
 
-constexpr int kScanU = 4;
+constexpr int kGradU = 4;
+constexpr int kRowTiles = 1024;  // of a row that one workgroup takes: kMarked columns of fp32
 
 // One workgroup per row.
 template <typename TI, typename TO, int NW, bool TAIL, bool GRAD>
 __global__ __launch_bounds__(NW * 64) void k_distill(Logits in, Logits grad, emu_teacher_t te, float c1, float* loss, float4* stats, uint64_t row0) {
   extern __shared__ uint32_t bits[];
   __shared__ DistillLds<NW> t;
+  __shared__ Listed<GRAD ? kRowTiles : 2> list;
   const uint64_t r = row0 + blockIdx.x;
   const float w = te.weight ? te.weight[r] : 1.0f;
   Entry e = {-1, 0.0f, -kInf};
   Stats st = kSkipped;
   bool none = false;
+  if constexpr (GRAD)
+    for (int i = threadIdx.x; i < kRowTiles; i += NW * 64) list.head[i] = -1;
   if (w != 0.0f) {
     float rest, value;
-    e = load_teacher<TI, NW>(t, te, r, in, 0, in.V, &rest, &none);
-    if constexpr (TAIL) mark_listed<NW>(bits, 0, (in.V + kScanU * kTile<TI> - 1) / (kScanU * kTile<TI>) * (kScanU * kTile<TI>), te, r, in.V);
-    const Running run = block_joined<NW>(scan<TI, kScanU, NW, TAIL, GRAD ? POL_PLAIN : POL_NT>(in, r * in.row_bytes, 0, in.V, c1, bits), t.run, c1);
+    const Stored f = fetch_teacher(te, r, in.V);
+    const Span row = {0, tiles<TI>(in.V)};
+    if constexpr (TAIL) mark_listed<NW>(bits, 0, row.t1 * kTile<TI>, f.col);
+    const Running run = block_joined<NW>(scan<TI, NW, TAIL, GRAD ? POL_PLAIN : POL_NT>(in, r * in.row_bytes, row, c1, bits), t.run, c1);
+    e = take_teacher<TI, NW>(t, f, te, r, in, 0, in.V, &rest, &none);
     st = finish<TI, NW, TAIL>(in, r * in.row_bytes, run, e, rest, te.k, c1, t, &value);
     write_row(loss, stats, r, value * w, st);
   } else {
     write_row(loss, stats, r, 0.0f, st);
   }
-  if constexpr (GRAD) row_gradient<TI, TO, kScanU, NW, POL_NT>(in, grad, r, 0, in.Vp, e, st, c1, w, none);
+  if constexpr (GRAD) row_gradient<TI, TO, kGradU, NW, POL_NT>(in, grad, r, {0, tiles<TI>(in.Vp)}, list, e, st, c1, w, none);
+}
+
+// A row held in the registers of 1,024 threads between its two uses, up to NV tiles of each wave, where the shards hold
+// whole vectors and are no shorter than a tile (a tile then lies in one shard or two): one read, one write. The
+// workgroups stay and take rows by ticket; while a vector's gradient leaves, the next row's vector is loaded into its
+// registers, so that memory has both to do. Tiles, and the order of every sum, are k_distill's: the result is
+// the same, bit for bit.
+constexpr int kRowWaves = 16;
+
+// What k_distill_resident needs of the teachers, a wave per row: per entry its column (-1: none, or one that an earlier
+// entry has) and that column's whole probability, per row the mass outside the list (-1: nothing listed). The
+// exponentials and comparisons stay out of the row's own way there. Also the first ticket.
+constexpr int kPrepareWaves = 4;
+struct Prepared {
+  Stored entry[kMaxTeacher];
+};
+__global__ __launch_bounds__(kPrepareWaves * 64) void k_prepare_teacher(emu_teacher_t te, uint32_t V, Prepared* out, float* rest, uint32_t* ticket,
+                                                                        uint32_t rows, uint64_t row0) {
+  __shared__ int32_t cols[kPrepareWaves][kMaxTeacher];
+  __shared__ double ps[kPrepareWaves][kMaxTeacher];
+  const uint32_t w = wave_id(), lane = threadIdx.x & 63, row = blockIdx.x * kPrepareWaves + w;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+  if (row >= rows) return;
+  const uint64_t r = row0 + row;
+  if (te.weight && te.weight[r] == 0.0f) return;
+  constexpr int N = kMaxTeacher / 64;
+  int32_t col[N];
+  double value[N], top = -double(kInf);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int j = i * 64 + lane;
+    col[i] = -1;
+    value[i] = -double(kInf);
+    if (j < te.k) {
+      const int32_t v = te.index[r * te.index_stride + j];
+      if (uint32_t(v) < V) {
+        col[i] = v;
+        value[i] = double(te.value[r * te.value_stride + j]);
+      }
+    }
+    top = fmax(top, value[i]);
+  }
+  top = wave_reduce(top, [](double a, double b) { return fmax(a, b); });
+  if (te.tail || top == -double(kInf)) top = 0.0;
+  double p[N], sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    p[i] = i * 64 < te.k && col[i] >= 0 ? exp(value[i] - top) : 0.0;
+    sum += wave_reduce(p[i], addd);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (!te.tail && sum != 0.0) p[i] /= sum;
+    cols[w][i * 64 + lane] = col[i];
+    ps[w][i * 64 + lane] = p[i];
+  }
+  wave_sync();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int j = i * 64 + lane;
+    if (j >= te.k) break;
+    bool first = col[i] >= 0;
+    for (int o = 0; o < te.k; ++o) {
+      if (o == j || cols[w][o] != col[i]) continue;
+      if (o < j) first = false;
+      else p[i] += ps[w][o];
+    }
+    out[row].entry[j] = first ? Stored{col[i], float(p[i])} : Stored{-1, 0.0f};
+  }
+  const float left = float(1.0 - sum);
+  if (lane == 0) rest[row] = te.tail ? (left < 0.0f ? 0.0f : left) : sum == 0.0 ? -1.0f : 0.0f;
+}
+
+template <typename TI, typename TO, int NV, bool TAIL>
+__global__ __launch_bounds__(kRowWaves * 64) void k_distill_resident(Logits in, Logits grad, emu_teacher_t te, float c1, float* loss, float4* stats,
+                                                                     const Prepared* teacher, const float* rests, uint32_t* ticket, uint32_t rows,
+                                                                     uint64_t row0) {
+  constexpr int NW = kRowWaves, U = kScanU;
+  constexpr uint32_t E = kE<TI>;
+  extern __shared__ uint32_t bits[];
+  __shared__ DistillLds<NW> t;
+  __shared__ Listed<NW * NV> list;
+  __shared__ Running inside_run[NW];
+  __shared__ uint32_t taken, first;
+  v4u x[NV];
+  uint32_t now = rows, next, after;  // the row in x, the row to load, the one behind it; `rows`: none
+  float w = 0.0f;
+  Entry e = {-1, 0.0f, -kInf};
+  if constexpr (TAIL)
+    for (uint32_t i = threadIdx.x; i < tiles<TI>(in.V) * kTile<TI> / 32; i += NW * 64) bits[i] = 0;
+  for (int i = threadIdx.x; i < NW * NV; i += NW * 64) list.head[i] = -1;
+  if (threadIdx.x == 0) first = atomicAdd(ticket, 1u);
+  __syncthreads();
+  next = umin(__builtin_amdgcn_readfirstlane(first), rows);
+  for (;;) {
+    const uint64_t r = row0 + now, ri = r * in.row_bytes;
+    // the tiles' places are the same in every turn: kept out of the compiler's sight, which would hold them all in registers
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const uint32_t lane = thread & 63;
+    const Span span = part_of({0, tiles<TI>(in.V)}, __builtin_amdgcn_readfirstlane(thread >> 6), NW);
+    const uint32_t t0 = span.t0, t1 = span.t1;
+    // what the turn needs beside x is on its way during the scan: a wait for it behind the loads would be one for them
+    uint32_t later = rows;
+    if (threadIdx.x == 0 && next < rows) later = atomicAdd(ticket, 1u);
+    const float w_next = next < rows ? (te.weight ? te.weight[row0 + next] : 1.0f) : 0.0f;
+    Stored f_next = {-1, 0.0f};
+    if (w_next != 0.0f && int(threadIdx.x) < te.k) f_next = teacher[next].entry[threadIdx.x];
+    Stats st = kSkipped;
+    float rest = 0.0f, rest_loss = 0.0f, scale = 0.0f, coef = 0.0f;
+    const bool live = now < rows && w != 0.0f;
+    if (live) {
+      if constexpr (TAIL) {
+        if (e.col >= 0) atomicOr(&bits[e.col / 32], 1u << (e.col % 32));
+        __syncthreads();
+      }
+      Running run = {-kInf, 0.0f};
+#pragma unroll
+      for (int i = 0; i < NV; i += U) {
+        if (t0 + i >= t1) break;
+        float f[U][E];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          asm volatile("" : "+v"(x[i + u]));  // in this order: all at once would take twice the registers
+          if constexpr (TAIL)
+            if (t0 + i + u < t1) leave_out<TI>(x[i + u], bits, (t0 + i + u) * kTile<TI> + lane * E);
+          unpack(x[i + u], f[u]);
+        }
+        add_values<U, E>(run, f, c1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      run = wave_joined(run, c1);
+      if (lane == 0) t.run[wave_id()] = run;
+      if constexpr (TAIL) {
+        const Running in_list = wave_joined(entry_run(e, c1), c1);
+        if (lane == 0) inside_run[wave_id()] = in_list;
+      }
+      if (int(threadIdx.x) < kMaxTeacher) t.col[threadIdx.x] = e.col;
+    }
+    rest = live ? rests[now] : 0.0f;
+    if (threadIdx.x == 0) taken = later;  // everyone has read the last one before the last turn's last barrier
+    __syncthreads();
+    after = umin(__builtin_amdgcn_readfirstlane(taken), rows);
+    if (live) {
+      Running all[NW], inside = {-kInf, 0.0f};
+#pragma unroll
+      for (int i = 0; i < NW; ++i) all[i] = t.run[i];
+      const Running run = joined(all, c1);
+      if constexpr (TAIL) {
+#pragma unroll
+        for (int i = 0; i < NW; ++i) all[i] = inside_run[i];
+        inside = joined(all, c1);
+        if (e.col >= 0) bits[e.col / 32] = 0;
+      }
+      st = conclude<TI, NW, TAIL>(in, ri, run, inside, e, rest < 0.0f ? 0.0f : rest, te.k, c1, t, &rest_loss);
+      scale = w * (c1 * 0.69314718f);
+    }
+    const uint64_t ro = r * grad.row_bytes, rn = (row0 + next) * in.row_bytes;
+    float z_next = -kInf;
+    if (f_next.col >= 0) z_next = widen(*column<TI>(in, rn, f_next.col));
+    const bool dead = !live || rest < 0.0f;
+    const bool zero = dead || st.s == 0.0f, wild = !zero && !plain(st.m, c1);
+    const float ref = reference(st.m, c1);
+    if (!zero) coef = scale * st.factor * ((wild ? 1.0f : __builtin_amdgcn_exp2f(-fmaf(st.m, c1, -ref))) / st.s);
+    int heads = -1;
+    if (!dead) {
+      chain<TI>(list, 0, e, entry_gradient(e, st, c1, scale));
+      __syncthreads();
+      if (t0 + lane < t1) heads = list.head[t0 + lane];
+    }
+    if (wild) dense_gradient<TI, TO, 1, NW, POL_NT, ANY_RANGE>(in, grad, r, {0, tiles<TI>(in.V)}, &list, st.m, c1, coef);
+    const bool write = now < rows && !wild;
+    Reader<TI> from(in, rn, t0);
+    Cursor<TO, kTile<TI>> to(grad, ro, t0);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (t0 + i >= t1) {
+        x[i] = (v4u){kMinusInf<TI>, kMinusInf<TI>, kMinusInf<TI>, kMinusInf<TI>};
+        continue;
+      }
+      if (write) {
+        float f[E];
+        if (zero) {
+#pragma unroll
+          for (uint32_t q = 0; q < E; ++q) f[q] = 0.0f;
+        } else {
+          asm volatile("" : "+v"(x[i]));  // unpacked anew: the scan's values would take twice the registers
+          unpack(x[i], f);
+#pragma unroll
+          for (uint32_t q = 0; q < E; ++q) f[q] = __builtin_amdgcn_exp2f(fmaf(f[q], c1, -ref)) * coef;
+          if (to.c + kTile<TI> > in.V) {
+#pragma unroll
+            for (uint32_t q = 0; q < E; ++q)
+              if (to.c + lane * E + q >= in.V) f[q] = 0.0f;
+          }
+        }
+        take_listed(list, __builtin_amdgcn_readlane(heads, i), to.c + lane * E, f);
+        store_tile<TO, POL_NT, E, true>(grad, to, lane, f);
+      }
+      if (w_next != 0.0f) {
+        if (from.one(in, 1)) x[i] = ld16_any<POL_NT>(from.base, lane * 16);
+        else x[i] = load_border<TI, POL_NT, true>(in, from, lane);
+      }
+      from.advance(in, 1);
+      to.advance(grad, 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float part = wave_reduce(live ? entry_loss(e, st, c1) : 0.0f, add);
+    if (lane == 0) t.sum[wave_id()] = part;
+    if (now < rows) {
+      __syncthreads();
+      if (!dead && e.col >= 0) list.head[e.col / kTile<TI>] = -1;
+      float total = t.sum[0];
+#pragma unroll
+      for (int i = 1; i < kMaxTeacher / 64; ++i) total += t.sum[i];
+      write_row(loss, stats, r, live ? (total + rest_loss) * w : 0.0f, st);
+    }
+    if (next >= rows) return;
+    now = next;
+    next = after;
+    w = w_next;
+    e = {f_next.col, f_next.value, z_next};
+  }
 }
 
 // Several workgroups per row: a part's statistics.
@@ -878,17 +1280,16 @@ __global__ __launch_bounds__(NW * 64) void k_distill_scan(Logits in, emu_teacher
   __shared__ Running run[NW];
   const uint64_t r = row0 + blockIdx.x;
   if (te.weight && te.weight[r] == 0.0f) return;
-  uint32_t c0, end;
-  part_range<TI, kScanU, NW>(in.V, blockIdx.y, gridDim.y, &c0, &end);
-  if constexpr (TAIL) mark_listed<NW>(bits, c0, (end - c0 + kScanU * kTile<TI> - 1) / (kScanU * kTile<TI>) * (kScanU * kTile<TI>), te, r, in.V);
-  const Running a = block_joined<NW>(scan<TI, kScanU, NW, TAIL, POL_PLAIN>(in, r * in.row_bytes, c0, end, c1, bits), run, c1);
+  const Span block = part_of({0, tiles<TI>(in.V)}, blockIdx.y, gridDim.y);
+  if constexpr (TAIL) mark_listed<NW>(bits, block.t0 * kTile<TI>, (block.t1 - block.t0) * kTile<TI>, fetch_teacher(te, r, in.V).col);
+  const Running a = block_joined<NW>(scan<TI, NW, TAIL, POL_PLAIN>(in, r * in.row_bytes, block, c1, bits), run, c1);
   if (threadIdx.x == 0) part[uint64_t(blockIdx.x) * gridDim.y + blockIdx.y] = a;
 }
 
 // The row's statistics and loss from its parts'.
 template <typename T, int NW, bool TAIL>
 __global__ __launch_bounds__(NW * 64) void k_distill_join(Logits in, emu_teacher_t te, float c1, float* loss, float4* stats,
-                                                          const Running* part, uint32_t parts, uint64_t row0) {
+                                                          const Running* part, uint32_t parts, Prepared* teacher, float* rests, uint64_t row0) {
   __shared__ DistillLds<NW> t;
   const uint64_t r = row0 + blockIdx.x;
   const uint32_t lane = threadIdx.x & 63;
@@ -896,37 +1297,51 @@ __global__ __launch_bounds__(NW * 64) void k_distill_join(Logits in, emu_teacher
   if (w == 0.0f) return write_row(loss, stats, r, 0.0f, kSkipped);
   float rest, value;
   bool none;
-  const Entry e = load_teacher<T, NW>(t, te, r, in, 0, in.V, &rest, &none);
+  const Entry e = take_teacher<T, NW>(t, fetch_teacher(te, r, in.V), te, r, in, 0, in.V, &rest, &none);
   const Running run = wave_joined(lane < parts ? part[uint64_t(blockIdx.x) * parts + lane] : Running{-kInf, 0.0f}, c1);
   const Stats st = finish<T, NW, TAIL>(in, r * in.row_bytes, run, e, rest, te.k, c1, t, &value);
   write_row(loss, stats, r, value * w, st);
+  if (int(threadIdx.x) < te.k) teacher[blockIdx.x].entry[threadIdx.x] = {e.col, e.p};
+  if (threadIdx.x == 0) rests[blockIdx.x] = none ? -1.0f : rest;
 }
 
-// The gradient of a row, or of a part of it, from the row's statistics.
+// The gradient of a part of a row, kBackwardTiles of it, from the row's statistics and prepared entries. Neighbouring
+// workgroups have neighbouring parts: the whole device then writes one front, where copies ran at 6.3 TB/s against 5.7
+// with a row per workgroup.
+constexpr uint32_t kBackwardTiles = 16;
 template <typename TI, typename TO, int NW>
-__global__ __launch_bounds__(NW * 64) void k_distill_backward(Logits in, Logits grad, emu_teacher_t te, float c1, const float4* stats, uint64_t row0) {
-  __shared__ DistillLds<NW> t;
-  const uint64_t r = row0 + blockIdx.x;
+__global__ __launch_bounds__(NW * 64) void k_distill_backward(Logits in, Logits grad, emu_teacher_t te, float c1, const float4* stats,
+                                                              const Prepared* teacher, const float* rests, uint32_t parts, uint64_t row0) {
+  static_assert(NW * 64 >= kMaxTeacher, "one entry per thread");
+  const uint32_t row = blockIdx.x / parts, part = blockIdx.x - row * parts;
+  const uint64_t r = row0 + row;
   const float w = te.weight ? te.weight[r] : 1.0f;
-  uint32_t c0, end;
-  part_range<TI, kScanU, NW>(in.Vp, blockIdx.y, gridDim.y, &c0, &end);
+  const Span block = {part * kBackwardTiles, umin((part + 1) * kBackwardTiles, tiles<TI>(in.Vp))};
+  __shared__ Listed<kBackwardTiles> list;
   Entry e = {-1, 0.0f, -kInf};
   Stats st = kSkipped;
   bool none = false;
+  if (threadIdx.x < kBackwardTiles) list.head[threadIdx.x] = -1;
   if (w != 0.0f) {
-    float rest;
-    e = load_teacher<TI, NW>(t, te, r, in, c0, end, &rest, &none);
     const float4 f = stats[r];
     st = {f.x, f.y, f.z, f.w};
+    none = rests[row] < 0.0f;
+    if (int(threadIdx.x) < te.k) {
+      const Stored f = teacher[row].entry[threadIdx.x];
+      const uint32_t tile = uint32_t(f.col) / kTile<TI>;
+      if (f.col >= 0 && tile >= block.t0 && tile < block.t1) e = {f.col, f.value, widen(*column<TI>(in, r * in.row_bytes, f.col))};
+    }
+    asm volatile("" ::"v"(e.z));  // read before anyone writes, in place, behind the barrier
+    __syncthreads();
   }
-  row_gradient<TI, TO, kScanU, NW, POL_NT>(in, grad, r, c0, end, e, st, c1, w, none);
+  row_gradient<TI, TO, kGradU, NW, POL_NT>(in, grad, r, block, list, e, st, c1, w, none);
 }
 
-// How many workgroups share a row: as many as fill the device with `wanted` workgroups, each with at least a chunk
-// per wave, and so many that a part's marks fit in LDS.
+// How many workgroups share a row: as many as fill the device with `wanted` workgroups, each with at least two
+// tiles per wave, and so many that a part's marks fit in LDS.
 constexpr uint32_t kMarked = 1u << 18;  // columns
 static uint32_t row_parts(const emu_logits_t* l, uint32_t V, int waves, int64_t wanted) {
-  const uint32_t unit = uint32_t(waves) * 4 * (l->dtype == EMU_BF16 ? kTile<bf16_t> : kTile<float>);
+  const uint32_t unit = uint32_t(waves) * 2 * (l->dtype == EMU_BF16 ? kTile<bf16_t> : kTile<float>);
   const uint32_t most = std::min((V + unit - 1) / unit, kMaxSplits);
   const int64_t want = l->rows ? (wanted + l->rows - 1) / l->rows : 1;
   return std::max(uint32_t(std::min<int64_t>(want, most)), (V + kMarked - 1) / kMarked);
@@ -1034,20 +1449,49 @@ static void by_types(int32_t in, int32_t out, F f) {
 }
 
 constexpr int kPartWaves = 4;  // of a workgroup that has a part of a row
-constexpr int kRowWaves = 8;   // of one that has a row
 
 static uint32_t topk_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kTopWaves, 1024); }
 static uint32_t distill_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kPartWaves, l->rows < 256 ? 1024 : 1); }
-static uint32_t backward_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kPartWaves, 2048); }
+
+// The workspace of the distillation calls.
+struct DistillWorkspace {
+  uint32_t* ticket;
+  float* rests;       // [rows]
+  Prepared* teacher;  // [rows]
+  Running* part;      // [rows][parts]
+  uint64_t bytes;
+  DistillWorkspace(void* at, uint64_t rows, uint64_t parts) {
+    uint8_t* p = static_cast<uint8_t*>(at);
+    ticket = reinterpret_cast<uint32_t*>(p);
+    rests = reinterpret_cast<float*>(p + 256);
+    teacher = reinterpret_cast<Prepared*>(p + 256 + (rows + 63) / 64 * 256);
+    part = reinterpret_cast<Running*>(teacher + rows);
+    bytes = 256 + (rows + 63) / 64 * 256 + rows * (sizeof(Prepared) + parts * sizeof(Running));
+  }
+};
+
+// The tiles of each wave in k_distill_resident, 0 where it does not take the row.
+constexpr int64_t kResidentRows = 256;
+template <typename T>
+static uint32_t resident_tiles(const Logits& l) {
+  const uint32_t per_wave = (tiles<T>(l.V) + kRowWaves - 1) / kRowWaves;
+  return l.cols % kE<T> == 0 && l.cols >= kTile<T> && tiles<T>(l.Vp) == tiles<T>(l.V) && per_wave <= 16 ? per_wave : 0;
+}
 
 template <typename TI>
-static void launch_backward(TI, int32_t dtype, uint32_t n, uint32_t parts, hipStream_t st, const Logits& li, const Logits& lo,
-                            const emu_teacher_t& te, float c1, const float4* stats, uint64_t r0) {
+static void launch_backward(TI, int32_t dtype, uint32_t n, hipStream_t st, const Logits& li, const Logits& lo, const emu_teacher_t& te, float c1,
+                            const float4* stats, const DistillWorkspace& ws, uint64_t r0) {
+  const uint32_t parts = (tiles<TI>(li.Vp) + kBackwardTiles - 1) / kBackwardTiles;
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(n, parts), dim3(kPartWaves * 64), 0, st, li, lo, te, c1, stats, r0);
+    hipLaunchKernelGGL(kernel, dim3(n * parts), dim3(kPartWaves * 64), 0, st, li, lo, te, c1, stats, ws.teacher, ws.rests, parts, r0);
   };
   if (dtype == EMU_BF16) launch(k_distill_backward<TI, bf16_t, kPartWaves>);
   else launch(k_distill_backward<TI, float, kPartWaves>);
+}
+
+static void launch_prepare(uint32_t n, hipStream_t st, const emu_teacher_t& te, uint32_t V, const DistillWorkspace& ws, uint64_t r0) {
+  hipLaunchKernelGGL(k_prepare_teacher, dim3((n + kPrepareWaves - 1) / kPrepareWaves), dim3(kPrepareWaves * 64), 0, st, te, V, ws.teacher, ws.rests,
+                     ws.ticket, n, r0);
 }
 
 }  // namespace emu
@@ -1064,7 +1508,7 @@ int emu_logits_workspace(const emu_logits_t* logits, int32_t k, uint64_t* bytes)
   if (k < 0 || k > kMaxTop) return fail(EMU_ERR_RANGE, "k %d not in [0, %d]", k, kMaxTop);
   const uint64_t rows = uint64_t(std::min<int64_t>(logits->rows, kRowsPerLaunch));
   const uint32_t parts = k ? topk_parts(logits, l.V) : distill_parts(logits, l.V);
-  *bytes = parts == 1 ? 0 : rows * parts * (sizeof(Running) + (k ? 64 * sizeof(uint64_t) : 0));
+  *bytes = k == 0 ? DistillWorkspace(nullptr, rows, parts).bytes : parts > 1 ? rows * parts * (sizeof(Running) + 64 * sizeof(uint64_t)) : 0;
   return EMU_OK;
 }
 
@@ -1154,27 +1598,45 @@ int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   drop_pending_error();
   const uint32_t parts = distill_parts(student, li.V);
+  const int n_cus = device_cus();
+  if (n_cus <= 0) return fail(EMU_ERR_HIP, "cannot query the current device");
+  const uint32_t cus = uint32_t(n_cus);
   float4* stats = reinterpret_cast<float4*>(d_stats);
-  Running* part = static_cast<Running*>(d_workspace);
   by_type(student->dtype, [&](auto ti) {
     using TI = decltype(ti);
-    constexpr uint32_t kChunk = kScanU * kTile<TI>;
-    const uint32_t chunks = (li.V + kChunk - 1) / kChunk;
-    const size_t marks = teacher->tail ? size_t((chunks + parts - 1) / parts) * kChunk / 8 : 0;
+    const uint32_t n_tiles = tiles<TI>(li.V), resident = grad && student->rows >= kResidentRows && parts == 1 ? resident_tiles<TI>(li) : 0;
+    const size_t marks = teacher->tail ? size_t((n_tiles + parts - 1) / parts) * kTile<TI> / 8 : 0;
     over_rows(student->rows, [&](uint64_t r0, uint32_t n) {
+      const DistillWorkspace ws(d_workspace, n, parts);
       auto by_tail = [&](auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
         if (parts > 1) {
-          hipLaunchKernelGGL((k_distill_scan<TI, kPartWaves, TAIL>), dim3(n, parts), dim3(kPartWaves * 64), marks, st, li, *teacher, c1, part, r0);
-          hipLaunchKernelGGL((k_distill_join<TI, kPartWaves, TAIL>), dim3(n), dim3(kPartWaves * 64), 0, st, li, *teacher, c1, d_loss, stats, part, parts, r0);
-          if (grad) launch_backward(ti, grad->dtype, n, parts, st, li, lo, *teacher, c1, stats, r0);
-        } else if (!grad) {
-          hipLaunchKernelGGL((k_distill<TI, TI, kRowWaves, TAIL, false>), dim3(n), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, r0);
-        } else if (grad->dtype == EMU_BF16) {
-          hipLaunchKernelGGL((k_distill<TI, bf16_t, kRowWaves, TAIL, true>), dim3(n), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, r0);
-        } else {
-          hipLaunchKernelGGL((k_distill<TI, float, kRowWaves, TAIL, true>), dim3(n), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, r0);
+          hipLaunchKernelGGL((k_distill_scan<TI, kPartWaves, TAIL>), dim3(n, parts), dim3(kPartWaves * 64), marks, st, li, *teacher, c1, ws.part, r0);
+          hipLaunchKernelGGL((k_distill_join<TI, kPartWaves, TAIL>), dim3(n), dim3(kPartWaves * 64), 0, st, li, *teacher, c1, d_loss, stats, ws.part,
+                             parts, ws.teacher, ws.rests, r0);
+          if (grad) launch_backward(ti, grad->dtype, n, st, li, lo, *teacher, c1, stats, ws, r0);
+          return;
         }
+        if (!grad) {
+          hipLaunchKernelGGL((k_distill<TI, TI, kRowWaves, TAIL, false>), dim3(n), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, r0);
+          return;
+        }
+        by_type(grad->dtype, [&](auto to) {
+          using TO = decltype(to);
+          if (!resident) {
+            hipLaunchKernelGGL((k_distill<TI, TO, kRowWaves, TAIL, true>), dim3(n), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, r0);
+            return;
+          }
+          launch_prepare(n, st, *teacher, li.V, ws, r0);
+          auto launch = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3(std::min(n, cus)), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, ws.teacher, ws.rests,
+                               ws.ticket, n, r0);
+          };
+          if (resident <= 4) launch(k_distill_resident<TI, TO, 4, TAIL>);
+          else if (resident <= 8) launch(k_distill_resident<TI, TO, 8, TAIL>);
+          else if (resident <= 12) launch(k_distill_resident<TI, TO, 12, TAIL>);
+          else launch(k_distill_resident<TI, TO, 16, TAIL>);
+        });
       };
       teacher->tail ? by_tail(std::true_type()) : by_tail(std::false_type());
     });
@@ -1195,10 +1657,12 @@ int emu_distill_backward(const emu_logits_t* student, const emu_teacher_t* teach
   if (student->rows == 0) return EMU_OK;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   drop_pending_error();
-  const uint32_t parts = backward_parts(student, li.Vp);
+  const uint32_t parts = distill_parts(student, li.V);
   by_type(student->dtype, [&](auto ti) {
     over_rows(student->rows, [&](uint64_t r0, uint32_t n) {
-      launch_backward(ti, grad->dtype, n, parts, st, li, lo, *teacher, c1, reinterpret_cast<const float4*>(d_stats), r0);
+      const DistillWorkspace ws(d_workspace, n, parts);
+      launch_prepare(n, st, *teacher, li.V, ws, r0);
+      launch_backward(ti, grad->dtype, n, st, li, lo, *teacher, c1, reinterpret_cast<const float4*>(d_stats), ws, r0);
     });
   });
   return hip_check("emu_distill_backward launch");
