@@ -48,6 +48,7 @@ __device__ __forceinline__ void st16(uint8_t* base, uint32_t off, v4u v) {
 }
 
 __device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
 typedef unsigned int v2u __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(1))) v2u gv2u;

@@ -33,6 +33,10 @@ __device__ __forceinline__ uint32_t shard_of(const Logits& l, uint32_t v) {
   return v - t * l.cols >= l.cols ? t + 1 : t;
 }
 
+// A value that the kernel does not write, at an address that is the same in every lane: by a scalar load, which
+// does not wait behind the vector loads in flight.
+template <typename T> __device__ __forceinline__ T scalar(const T* p) { return *(const __attribute__((address_space(4))) T*)p; }
+
 // ------------------------------------------------------------------------------------------------
 // rows in vectors
 // ------------------------------------------------------------------------------------------------
@@ -109,6 +113,23 @@ __device__ __forceinline__ Span part_of(Span s, uint32_t part, uint32_t parts) {
 __device__ __forceinline__ uint32_t wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 template <typename T> __host__ __device__ constexpr uint32_t tiles(uint32_t columns) { return (columns + kTile<T> - 1) / kTile<T>; }
 
+// load_edge by a table of the row's starts.
+template <typename T>
+__device__ __forceinline__ v4u load_lane(const Logits& l, const uint8_t* const* shard, uint32_t v) {
+  const uint32_t t = shard_of(l, v), lo = v - t * l.cols;
+  if (lo + kE<T> <= l.cols && v + kE<T> <= l.V) return ld16_any<POL_PLAIN>(shard[t], lo * uint32_t(sizeof(T)));
+  v4u x = {kMinusInf<T>, kMinusInf<T>, kMinusInf<T>, kMinusInf<T>};
+#pragma unroll
+  for (uint32_t e = 0; e < kE<T>; ++e) {
+    if (v + e >= l.V) break;
+    const uint32_t at = shard_of(l, v + e);
+    const T y = reinterpret_cast<const T*>(shard[at])[v + e - at * l.cols];
+    if constexpr (sizeof(T) == 2) x[e / 2] = e % 2 ? (x[e / 2] & 0xffffu) | uint32_t(y) << 16 : (x[e / 2] & 0xffff0000u) | y;
+    else x[e] = __float_as_uint(y);
+  }
+  return x;
+}
+
 // Where a wave is in its row: column c, in shard t at column lo, at `base`. TILE: the tile's columns. Going on keeps
 // the shard's address; finding it anew (a load from the arguments) is for the few tiles that begin in another shard.
 template <typename T, uint32_t TILE>
@@ -138,6 +159,7 @@ struct Cursor {
   __device__ __forceinline__ uint8_t* other(const Logits& l) const { return l.p[umin(t + 1, kMaxShards - 1)] + row_off - uint64_t(l.cols - lo) * sizeof(T); }
 };
 template <typename T> using Reader = Cursor<T, kTile<T>>;
+constexpr int kScanU = 2;  // tiles that a wave adds up at a time
 
 // A tile that is not wholly in one shard and below V. Where shards are no shorter than a tile it lies in two at
 // most, and only a vector across their border goes by element (WHOLE: there is none).
@@ -296,22 +318,16 @@ struct Running {
 __device__ __forceinline__ float reference(float m, float c1) { return fmaxf(m * c1, -kPlainRange); }
 __device__ __forceinline__ bool plain(float m, float c1) { return fabsf(m * c1) < kPlainRange; }
 
-// n statistics to one: relative to the largest maximum, summed in order.
-template <int N>
-__device__ __forceinline__ Running joined(const Running (&a)[N], float c1) {
-  Running j = a[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) j.m = fmaxf(j.m, a[i].m);
-  const float ref = reference(j.m, c1);
-  j.s = 0.0f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) j.s += a[i].s * __builtin_amdgcn_exp2f(reference(a[i].m, c1) - ref);
-  return j;
-}
-
 __device__ __forceinline__ Running wave_joined(Running a, float c1) {
   const float m = wave_reduce(a.m, [](float x, float y) { return fmaxf(x, y); });
   return {m, wave_reduce(a.s * __builtin_amdgcn_exp2f(reference(a.m, c1) - reference(m, c1)), add)};
+}
+
+// Of the workgroup's waves, from LDS.
+template <int NW>
+__device__ __forceinline__ Running waves_joined(const Running* lds, float c1) {
+  const uint32_t lane = threadIdx.x & 63;
+  return wave_joined(lane < NW ? lds[lane] : Running{-kInf, 0.0f}, c1);
 }
 
 // Over the workgroup, in every thread. lds must not be in use: the caller has passed a barrier since it was.
@@ -320,20 +336,18 @@ __device__ __forceinline__ Running block_joined(Running a, Running* lds, float c
   a = wave_joined(a, c1);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
   __syncthreads();
-  Running all[NW];
-#pragma unroll
-  for (int w = 0; w < NW; ++w) all[w] = lds[w];
-  return joined(all, c1);
+  return waves_joined<NW>(lds, c1);
 }
 
-// U vectors of a lane.
+// U vectors of a lane; gives their largest value.
 template <int U, uint32_t E>
-__device__ __forceinline__ void add_values(Running& r, const float (&f)[U][E], float c1) {
-  float m = r.m;
+__device__ __forceinline__ float add_values(Running& r, const float (&f)[U][E], float c1) {
+  float top = f[0][0];
 #pragma unroll
   for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (uint32_t e = 0; e < E; e += 2) m = max3(m, f[u][e], f[u][e + 1]);
+    for (uint32_t e = 0; e < E; e += 2) top = max3(top, f[u][e], f[u][e + 1]);
+  const float m = fmaxf(r.m, top);
   const float ref = reference(m, c1);
   float s = 0.0f;
 #pragma unroll
@@ -342,6 +356,7 @@ __device__ __forceinline__ void add_values(Running& r, const float (&f)[U][E], f
     for (uint32_t e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(f[u][e], c1, -ref));
   r.s = r.s * __builtin_amdgcn_exp2f(reference(r.m, c1) - ref) + s;
   r.m = m;
+  return top;
 }
 
 // exp(m / tau) * the result is the sum of exp(x / tau) behind r, for a maximum in the plain range.
@@ -531,46 +546,51 @@ __global__ __launch_bounds__(kConstrainThreads) void k_constrain(Logits in, Logi
 // ------------------------------------------------------------------------------------------------
 // the k largest
 // ------------------------------------------------------------------------------------------------
-// Every logit has a key whose order is the result's: the value, then the lower column. Each wave keeps its k
-// largest keys sorted, one per lane, beside the softmax statistics of the same pass. Logits above the k-th are
-// collected in LDS and merged in 64 at a time (a bitonic sort across the lanes and one merge); the k-th key is
-// shared with the row's other waves, so that a row admits about k log(V) logits. The first bound is the k-th
-// largest of the lanes' maxima over the wave's first tiles. The result does not depend on when a wave sees a
-// shared bound: a bound only ever drops keys that k others beat.
+// Every logit has a key whose order is the result's: the value, then the lower column. The scan for the softmax
+// statistics also gives every thread's largest logit, and its largest in each of up to kSegments stretches. The k-th
+// largest of the threads' maxima is a bound that k logits reach; about k + k^2 / (2 threads) do in all, in as many
+// stretches. Those stretches are read again by their lanes, and what reaches the bound is sorted. Where that is more
+// than the LDS list holds (ties at the bound, a few threads with all large logits), each wave goes over its tiles again
+// with its own k best sorted, one per lane, and merges in what beats its k-th, 64 at a time.
 
-__device__ __forceinline__ uint64_t top_key(float x, uint32_t v) {  // 0: never chosen
-  if (!(x > -kInf)) return 0;
+__device__ __forceinline__ uint32_t top_order(float x) {  // 0: never chosen
   const uint32_t u = __float_as_uint(x + 0.0f);  // -0 becomes 0
-  const uint32_t order = u & 0x80000000u ? ~u : u | 0x80000000u;
-  return uint64_t(order) << 32 | uint32_t(~v);
+  return x > -kInf ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 0;
 }
-__device__ __forceinline__ float key_value(uint64_t key) {
-  const uint32_t order = uint32_t(key >> 32);
-  return key == 0 ? -kInf : __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
+__device__ __forceinline__ uint64_t top_key(float x, uint32_t v) {
+  const uint32_t order = top_order(x);
+  return order ? uint64_t(order) << 32 | uint32_t(~v) : 0;
 }
+__device__ __forceinline__ float order_value(uint32_t order) {
+  return order == 0 ? -kInf : __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
+}
+__device__ __forceinline__ float key_value(uint64_t key) { return order_value(uint32_t(key >> 32)); }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
 __device__ __forceinline__ uint64_t lane_key(uint64_t x, uint32_t lane) {  // the same lane everywhere
   return uint64_t(__builtin_amdgcn_readlane(uint32_t(x >> 32), lane)) << 32 | uint32_t(__builtin_amdgcn_readlane(uint32_t(x), lane));
 }
 
-template <uint32_t K, uint32_t J>
-__device__ __forceinline__ uint64_t sort_step(uint64_t x) {  // larger ones to the lanes without bit J, in blocks of K by turns
+template <uint32_t K, uint32_t J, typename T>
+__device__ __forceinline__ T sort_step(T x) {  // larger ones to the lanes without bit J, in blocks of K by turns
   const uint32_t lane = threadIdx.x & 63;
-  const uint64_t y = lane_xor<J>(x);
-  return ((lane & J) == 0) == ((lane & K) == 0) ? max64(x, y) : min64(x, y);
+  const T y = lane_xor<J>(x);
+  const bool larger = x > y;
+  return (((lane & J) == 0) == ((lane & K) == 0)) == larger ? x : y;
 }
-template <uint32_t K, uint32_t J = K / 2>
-__device__ __forceinline__ uint64_t sort_steps(uint64_t x) {
+template <uint32_t K, uint32_t J = K / 2, typename T>
+__device__ __forceinline__ T sort_steps(T x) {
   x = sort_step<K, J>(x);
   if constexpr (J > 1) return sort_steps<K, J / 2>(x);
   return x;
 }
-__device__ __forceinline__ uint64_t sorted(uint64_t x) {  // across the wave, largest in lane 0
+template <typename T>
+__device__ __forceinline__ T sorted(T x) {  // across the wave, largest in lane 0
   return sort_steps<64>(sort_steps<32>(sort_steps<16>(sort_steps<8>(sort_steps<4>(sort_steps<2>(x))))));
 }
-__device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b) {  // the 64 largest of two sorted waves, sorted
-  return sort_steps<64>(max64(a, __shfl((unsigned long long)b, 63 - (threadIdx.x & 63))));
+template <typename T>
+__device__ __forceinline__ T merged(T a, T b_reversed) {  // the 64 largest of two sorted waves, sorted; the second with its smallest in lane 0
+  return sort_steps<64>(a > b_reversed ? a : b_reversed);
 }
 
 // What the wave's lanes wrote to LDS is what its lanes read from here on.
@@ -580,23 +600,36 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+constexpr int kSegments = 8;
 template <int NW>
 struct TopLds {
-  uint64_t fresh[NW][128];       // a wave's collected keys
-  uint64_t list[NW][64];
-  unsigned long long bound;      // the largest k-th key of any wave
+  union {
+    float segment[kSegments][NW * 64];  // the threads' maxima by stretch
+    uint64_t fresh[NW][128];            // the slow way: a wave's collected keys
+  };
+  uint64_t list[NW * 64];
+  uint32_t order[NW * 64];              // the threads' maxima; then the stretches to be read, thread | stretch << 16
+  uint32_t n, n_stretches;              // keys in the list, stretches
+  const uint8_t* shard[kMaxShards];     // the row's start in each
   Running run[NW];
   float sum[NW];
 };
 
-// The waves' lists to one, in wave 0.
-template <int NW>
-__device__ __forceinline__ uint64_t block_merged(uint64_t best, TopLds<NW>& t) {
-  const uint32_t lane = threadIdx.x & 63, w = wave_id();
-  t.list[w][lane] = best;
-  __syncthreads();
-  if (w == 0)
-    for (int i = 1; i < NW; ++i) best = merged(best, t.list[i][lane]);
+// The sorted lists of n waves to one, in wave 0 and in LDS.
+template <typename T>
+__device__ __forceinline__ T block_merged(T best, T* list, int n) {
+  const uint32_t lane = threadIdx.x & 63;
+  const int w = int(wave_id());
+  if (w < n) list[w * 64 + lane] = best;
+  while (n > 1) {
+    __syncthreads();
+    const int half = (n + 1) / 2;
+    if (w + half < n) {
+      best = merged(best, list[(w + half) * 64 + 63 - lane]);
+      list[w * 64 + lane] = best;
+    }
+    n = half;
+  }
   return best;
 }
 
@@ -618,83 +651,139 @@ __device__ __forceinline__ float row_sum(const Logits& l, uint64_t row_off, Runn
   return careful_sum<T, NW>(l, row_off, a.m, c1, nullptr, 0, lds);
 }
 
-constexpr int kTopWaves = 4;
-constexpr int kTopU = 4;
+__device__ __forceinline__ uint64_t reversed(uint64_t x) { return __shfl((unsigned long long)x, 63 - (threadIdx.x & 63)); }
 
-// Grid: rows, parts. One part: the row's result. More: the part's statistics and keys, for k_topk_join.
-template <typename T>
-__global__ __launch_bounds__(kTopWaves * 64) void k_topk(Logits in, uint32_t k, float c1, int32_t* index, float* logprob,
-                                                         float* lse, Running* part_run, uint64_t* part_keys, uint64_t row0) {
-  constexpr int NW = kTopWaves, U = kTopU;
+// The slow way: the wave's k largest keys among those >= bound, sorted.
+template <typename T, int NW>
+__device__ __forceinline__ uint64_t wave_top(const Logits& l, uint64_t off, Span span, uint32_t k, uint64_t bound, uint64_t (*fresh)[128]) {
   constexpr uint32_t E = kE<T>;
-  __shared__ TopLds<NW> t;
-  const uint64_t r = row0 + blockIdx.x, off = r * in.row_bytes;
   const uint32_t lane = threadIdx.x & 63, w = wave_id();
-  const Span span = part_of(part_of({0, tiles<T>(in.V)}, blockIdx.y, gridDim.y), w, NW);
-  if (threadIdx.x == 0) t.bound = 0;
-  __syncthreads();
-  uint64_t best = 0, bound = 0;  // every key in the row's result is >= bound
-  uint32_t n = 0;                // collected
+  uint64_t best = 0;
+  uint32_t n = 0;
   auto flush = [&](uint32_t have) {
     wave_sync();
-    const uint64_t x = sorted(lane < have ? t.fresh[w][lane] : 0);
-    best = merged(best, x);
+    best = merged(best, reversed(sorted(lane < have ? fresh[w][lane] : uint64_t(0))));
     const uint64_t kth = lane_key(best, k - 1);
-    if (lane == 0) atomicMax(&t.bound, (unsigned long long)kth);
-    bound = max64(bound, kth);
+    bound = max64(bound, kth + (kth != 0));  // from here on above it
   };
-  Running run = {-kInf, 0.0f};
-  bool first = true;
-  Reader<T> at(in, off, span.t0);
-  for (uint32_t tile = span.t0; tile < span.t1; tile += U) {
-    const uint32_t c = tile * kTile<T>;
-    v4u x[U];
-    load_tiles<T, U, POL_NT>(in, at, span.t1, x);
-    float f[U][E], top[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      unpack(x[u], f[u]);
-      top[u] = f[u][0];
-#pragma unroll
-      for (uint32_t e = 1; e < E; e += 2) top[u] = e + 1 < E ? max3(top[u], f[u][e], f[u][e + 1]) : max3(top[u], f[u][e], f[u][e]);
-    }
-    add_values<U, E>(run, f, c1);
-    if (first) {
-      float m = top[0];
-#pragma unroll
-      for (int u = 1; u < U; ++u) m = max3(m, top[u], top[u]);
-      bound = lane_key(sorted(top_key(m, ~0u)), k - 1);  // the lanes' maxima as if behind the last column
-      first = false;
-    }
-    bound = max64(bound, lane_key(__hip_atomic_load(&t.bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP), 0));
-    float level = key_value(bound);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (__all(top[u] < level)) continue;  // a NaN goes on
-#pragma unroll
-      for (uint32_t e = 0; e < E; ++e) {
-        const uint64_t key = top_key(f[u][e], c + u * kTile<T> + lane * E + e);
-        const uint64_t lanes = __ballot(key > bound);
-        if (!lanes) continue;
-        if (key > bound) t.fresh[w][n + __popcll(lanes & ((1ull << lane) - 1))] = key;
-        n += __popcll(lanes);
-        if (n >= 64) {
-          flush(64);
-          n -= 64;
-          const uint64_t left = t.fresh[w][64 + lane];
-          wave_sync();
-          t.fresh[w][lane] = left;
-          wave_sync();
-          level = key_value(bound);
-        }
+  Reader<T> at(l, off, span.t0);
+  for (uint32_t tile = span.t0; tile < span.t1; ++tile) {
+    v4u x[1];
+    const uint32_t c = at.c;
+    load_tiles<T, 1, POL_PLAIN>(l, at, span.t1, x);
+    float f[E];
+    unpack(x[0], f);
+    for (uint32_t e = 0; e < E; ++e) {
+      const uint64_t key = top_key(f[e], c + lane * E + e);
+      const uint64_t lanes = __ballot(key != 0 && key >= bound);
+      if (!lanes) continue;
+      if (key != 0 && key >= bound) fresh[w][n + __popcll(lanes & ((1ull << lane) - 1))] = key;
+      n += __popcll(lanes);
+      if (n >= 64) {
+        flush(64);
+        n -= 64;
+        const uint64_t left = fresh[w][64 + lane];
+        wave_sync();
+        fresh[w][lane] = left;
+        wave_sync();
       }
     }
   }
   if (n) flush(n);
+  return best;
+}
+
+constexpr int kTopParts = 4;  // waves of a workgroup that has a part of a row
+
+// A workgroup per part of a row, blockIdx.x = row * parts + part. One part: the row's result. More: the part's
+// statistics and keys, for k_topk_join.
+template <typename T, int NW>
+__global__ __launch_bounds__(NW * 64) void k_topk(Logits in, uint32_t k, float c1, int32_t* index, float* logprob, float* lse, Running* part_run,
+                                                  uint64_t* part_keys, uint32_t parts, uint64_t row0) {
+  constexpr int U = kScanU;
+  constexpr uint32_t E = kE<T>;
+  __shared__ TopLds<NW> t;
+  const uint32_t row = blockIdx.x / parts;
+  const uint64_t r = row0 + row, off = r * in.row_bytes;
+  const uint32_t lane = threadIdx.x & 63, w = wave_id();
+  const Span block = part_of({0, tiles<T>(in.V)}, blockIdx.x - row * parts, parts), span = part_of(block, w, NW);
+  const uint32_t per = (span.t1 - span.t0 + U * kSegments - 1) / (U * kSegments) * U;  // tiles of a stretch
+  if (threadIdx.x == 0) t.n = t.n_stretches = 0;
+  if (threadIdx.x < kMaxShards) t.shard[threadIdx.x] = in.p[threadIdx.x] + off;
+  Running run = {-kInf, 0.0f};
+  {
+    v4u x[U];
+    Reader<T> at(in, off, span.t0);
+    if (span.t0 < span.t1) load_tiles<T, U, POL_PLAIN>(in, at, span.t1, x);
+    float top = -kInf;
+    uint32_t segment = 0, segment_end = span.t0 + per;
+    for (uint32_t tile = span.t0; tile < span.t1; tile += U) {
+      v4u y[U];
+      if (tile + U < span.t1) load_tiles<T, U, POL_PLAIN>(in, at, span.t1, y);
+      float f[U][E];
+#pragma unroll
+      for (int u = 0; u < U; ++u) unpack(x[u], f[u]);
+      top = fmaxf(top, add_values<U, E>(run, f, c1));
+      if (tile + U >= segment_end || tile + U >= span.t1) {
+        t.segment[segment][threadIdx.x] = top;
+        ++segment;
+        segment_end += per;
+        top = -kInf;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = y[u];
+    }
+  }
+  // the k-th largest of the threads' maxima
+  block_merged(sorted(top_order(run.m)), t.order, NW);
   run = block_joined<NW>(run, t.run, c1);
-  best = block_merged<NW>(best, t);
-  if (gridDim.y > 1) {
-    const uint64_t at = (r - row0) * gridDim.y + blockIdx.y;
+  const uint32_t kth = t.order[k - 1];
+  const float level = order_value(kth);
+  __syncthreads();
+  // the stretches that hold what reaches it, and from them, a vector a thread, what does
+  const uint32_t stretches = per ? (span.t1 - span.t0 + per - 1) / per : 0;
+  for (uint32_t i = 0; i < stretches; ++i)
+    if (!(t.segment[i][threadIdx.x] < level)) {
+      const uint32_t pos = atomicAdd(&t.n_stretches, 1u);
+      if (pos < NW * 64) t.order[pos] = threadIdx.x | i << 16;
+    }
+  __syncthreads();
+  const uint32_t most = part_of(block, 0, NW).t1 - block.t0, longest = (most + U * kSegments - 1) / (U * kSegments) * U;  // the first wave's
+  const uint32_t n_vectors = t.n_stretches <= NW * 64 ? t.n_stretches * longest : 0;
+  for (uint32_t q = threadIdx.x; q < n_vectors; q += NW * 64) {
+    const uint32_t item = t.order[q / longest], thread = item & 0xffffu;
+    const Span its = part_of(block, thread >> 6, NW);
+    const uint32_t its_per = (its.t1 - its.t0 + U * kSegments - 1) / (U * kSegments) * U;
+    const uint32_t in_it = q % longest, tile = its.t0 + (item >> 16) * its_per + in_it;
+    if (in_it >= its_per || tile >= its.t1) continue;
+    const uint32_t v = tile * kTile<T> + (thread & 63) * E;
+    float f[E];
+    unpack(load_lane<T>(in, t.shard, v), f);
+#pragma unroll
+    for (uint32_t e = 0; e < E; ++e) {
+      const uint64_t key = f[e] >= level ? top_key(f[e], v + e) : 0;
+      if (key) {
+        const uint32_t pos = atomicAdd(&t.n, 1u);
+        if (pos < NW * 64) t.list[pos] = key;
+      }
+    }
+  }
+  __syncthreads();
+  const uint32_t n = t.n;
+  uint64_t best;
+  if (t.n_stretches <= NW * 64 && n <= NW * 64) {
+    const int lists = umax((n + 63) / 64, 1);
+    best = threadIdx.x < n ? t.list[threadIdx.x] : 0;
+    __syncthreads();
+    if (int(w) < lists) best = sorted(best);
+    best = block_merged(best, t.list, lists);
+  } else {
+    best = wave_top<T, NW>(in, off, span, k, uint64_t(kth) << 32, t.fresh);
+    __syncthreads();
+    best = block_merged(best, t.list, NW);
+  }
+  if (parts > 1) {
+    const uint64_t at = blockIdx.x;
     if (w == 0) part_keys[at * 64 + lane] = best;
     if (threadIdx.x == 0) part_run[at] = run;
     return;
@@ -705,17 +794,17 @@ __global__ __launch_bounds__(kTopWaves * 64) void k_topk(Logits in, uint32_t k, 
 
 // The parts of a row to its result.
 template <typename T>
-__global__ __launch_bounds__(kTopWaves * 64) void k_topk_join(Logits in, uint32_t k, float c1, int32_t* index, float* logprob,
+__global__ __launch_bounds__(kTopParts * 64) void k_topk_join(Logits in, uint32_t k, float c1, int32_t* index, float* logprob,
                                                               float* lse, const Running* part_run, const uint64_t* part_keys,
                                                               uint32_t parts, uint64_t row0) {
-  constexpr int NW = kTopWaves;
+  constexpr int NW = kTopParts;
   __shared__ TopLds<NW> t;
   const uint64_t r = row0 + blockIdx.x, at = uint64_t(blockIdx.x) * parts;
   const uint32_t lane = threadIdx.x & 63, w = wave_id();
   const Running run = wave_joined(lane < parts ? part_run[at + lane] : Running{-kInf, 0.0f}, c1);
   uint64_t best = 0;
-  for (uint32_t i = w; i < parts; i += NW) best = merged(best, part_keys[(at + i) * 64 + lane]);
-  best = block_merged<NW>(best, t);
+  for (uint32_t i = w; i < parts; i += NW) best = merged(best, part_keys[(at + i) * 64 + 63 - lane]);
+  best = block_merged(best, t.list, NW);
   const float s = row_sum<T, NW>(in, r * in.row_bytes, run, c1, t.sum);
   if (w == 0) write_top(best, k, run.m, s, c1, index, logprob, lse, r);
 }
@@ -825,7 +914,6 @@ __device__ __forceinline__ void leave_out(v4u& x, const uint32_t* bits, uint32_t
 
 // The wave's statistics of its part of the workgroup's span, without the marked columns if TAIL. The next tiles
 // are on their way while these are added up.
-constexpr int kScanU = 2;
 template <typename T, int NW, bool TAIL, int POL>
 __device__ __forceinline__ Running scan(const Logits& l, uint64_t off, Span block, float c1, const uint32_t* bits) {
   constexpr int U = kScanU;
@@ -1022,42 +1110,7 @@ constexpr Stats kSkipped = {__builtin_nanf(""), __builtin_nanf(""), __builtin_na
 constexpr int kGradU = 4;
 constexpr int kRowTiles = 1024;  // of a row that one workgroup takes: kMarked columns of fp32
 
-// One workgroup per row.
-template <typename TI, typename TO, int NW, bool TAIL, bool GRAD>
-__global__ __launch_bounds__(NW * 64) void k_distill(Logits in, Logits grad, emu_teacher_t te, float c1, float* loss, float4* stats, uint64_t row0) {
-  extern __shared__ uint32_t bits[];
-  __shared__ DistillLds<NW> t;
-  __shared__ Listed<GRAD ? kRowTiles : 2> list;
-  const uint64_t r = row0 + blockIdx.x;
-  const float w = te.weight ? te.weight[r] : 1.0f;
-  Entry e = {-1, 0.0f, -kInf};
-  Stats st = kSkipped;
-  bool none = false;
-  if constexpr (GRAD)
-    for (int i = threadIdx.x; i < kRowTiles; i += NW * 64) list.head[i] = -1;
-  if (w != 0.0f) {
-    float rest, value;
-    const Stored f = fetch_teacher(te, r, in.V);
-    const Span row = {0, tiles<TI>(in.V)};
-    if constexpr (TAIL) mark_listed<NW>(bits, 0, row.t1 * kTile<TI>, f.col);
-    const Running run = block_joined<NW>(scan<TI, NW, TAIL, GRAD ? POL_PLAIN : POL_NT>(in, r * in.row_bytes, row, c1, bits), t.run, c1);
-    e = take_teacher<TI, NW>(t, f, te, r, in, 0, in.V, &rest, &none);
-    st = finish<TI, NW, TAIL>(in, r * in.row_bytes, run, e, rest, te.k, c1, t, &value);
-    write_row(loss, stats, r, value * w, st);
-  } else {
-    write_row(loss, stats, r, 0.0f, st);
-  }
-  if constexpr (GRAD) row_gradient<TI, TO, kGradU, NW, POL_NT>(in, grad, r, {0, tiles<TI>(in.Vp)}, list, e, st, c1, w, none);
-}
-
-// A row held in the registers of 1,024 threads between its two uses, up to NV tiles of each wave, where the shards hold
-// whole vectors and are no shorter than a tile (a tile then lies in one shard or two): one read, one write. The
-// workgroups stay and take rows by ticket; while a vector's gradient leaves, the next row's vector is loaded into its
-// registers, so that memory has both to do. Tiles, and the order of every sum, are k_distill's: the result is
-// the same, bit for bit.
-constexpr int kRowWaves = 16;
-
-// What k_distill_resident needs of the teachers, a wave per row: per entry its column (-1: none, or one that an earlier
+// What the kernels need of the teachers, a wave per row: per entry its column (-1: none, or one that an earlier
 // entry has) and that column's whole probability, per row the mass outside the list (-1: nothing listed). The
 // exponentials and comparisons stay out of the row's own way there. Also the first ticket.
 constexpr int kPrepareWaves = 4;
@@ -1121,24 +1174,85 @@ __global__ __launch_bounds__(kPrepareWaves * 64) void k_prepare_teacher(emu_teac
   if (lane == 0) rest[row] = te.tail ? (left < 0.0f ? 0.0f : left) : sum == 0.0 ? -1.0f : 0.0f;
 }
 
-template <typename TI, typename TO, int NV, bool TAIL>
-__global__ __launch_bounds__(kRowWaves * 64) void k_distill_resident(Logits in, Logits grad, emu_teacher_t te, float c1, float* loss, float4* stats,
+// One workgroup per row.
+template <typename TI, typename TO, int NW, bool TAIL, bool GRAD>
+__global__ __launch_bounds__(NW * 64) void k_distill(Logits in, Logits grad, emu_teacher_t te, float c1, float* loss, float4* stats,
+                                                     const Prepared* teacher, const float* rests, uint64_t row0) {
+  extern __shared__ uint32_t bits[];
+  __shared__ DistillLds<NW> t;
+  __shared__ Listed<GRAD ? kRowTiles : 2> list;
+  const uint64_t r = row0 + blockIdx.x, off = r * in.row_bytes;
+  const float w = te.weight ? te.weight[r] : 1.0f;
+  Entry e = {-1, 0.0f, -kInf};
+  Stats st = kSkipped;
+  float rest = 0.0f;
+  if constexpr (GRAD)
+    for (int i = threadIdx.x; i < kRowTiles; i += NW * 64) list.head[i] = -1;
+  if (w != 0.0f) {
+    Stored f = {-1, 0.0f};
+    if (int(threadIdx.x) < te.k) f = teacher[blockIdx.x].entry[threadIdx.x];
+    const Span row = {0, tiles<TI>(in.V)};
+    if constexpr (TAIL) mark_listed<NW>(bits, 0, row.t1 * kTile<TI>, f.col);
+    const Running run = block_joined<NW>(scan<TI, NW, TAIL, GRAD ? POL_PLAIN : POL_NT>(in, off, row, c1, bits), t.run, c1);
+    e = {f.col, f.value, -kInf};
+    if (e.col >= 0) e.z = widen(*column<TI>(in, off, e.col));
+    if (int(threadIdx.x) < kMaxTeacher) t.col[threadIdx.x] = e.col;
+    rest = rests[blockIdx.x];
+    float value;
+    st = finish<TI, NW, TAIL>(in, off, run, e, rest < 0.0f ? 0.0f : rest, te.k, c1, t, &value);
+    write_row(loss, stats, r, value * w, st);
+  } else {
+    write_row(loss, stats, r, 0.0f, st);
+  }
+  if constexpr (GRAD) row_gradient<TI, TO, kGradU, NW, POL_NT>(in, grad, r, {0, tiles<TI>(in.Vp)}, list, e, st, c1, w, rest < 0.0f);
+}
+
+// A row held in registers between its two uses, up to NV tiles of each of NW waves, where the shards hold whole aligned
+// vectors and are no shorter than a tile (a tile then lies in one shard or two): one read, one write. The
+// workgroups stay and take rows by ticket, so that the device works on a window of neighbouring rows (in equal shares
+// fixed ahead, 4,096 rows of 131,072 took 450 us against 425) and rows without a weight cost no one more; while a vector's gradient leaves, the next row's vector is loaded into its
+// registers, so that memory has both to do. Every turn issues the same loads and stores, whatever the row: a wait
+// for one of them can then name the number of younger ones, where with any in doubt it would be for all. Tiles that
+// a wave does not have, and rows without a weight, load a vector of -infinities; a store beyond a shard's row is
+// dropped by the buffer's bounds. Tiles, and the order of every sum, are k_distill's: the result is the same, bit for bit.
+constexpr int kResidentTiles = 16;
+__device__ const v4u kNoLogits[2] = {{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}, {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}};
+
+// N columns a lane at byte `off` of the buffer; beyond its end nothing is written.
+template <typename TO, uint32_t N>
+__device__ __forceinline__ void store_bounded(__amdgpu_buffer_rsrc_t to, uint32_t off, const float (&f)[N]) {
+  constexpr int kStream = 2;  // nt
+  if constexpr (sizeof(TO) == 4) {
+#pragma unroll
+    for (uint32_t i = 0; i < N; i += 4)
+      __builtin_amdgcn_raw_buffer_store_b128((v4u){__float_as_uint(f[i]), __float_as_uint(f[i + 1]), __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3])}, to, off + i * 4, 0, kStream);
+  } else if constexpr (N == 8) {
+    __builtin_amdgcn_raw_buffer_store_b128((v4u){pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])}, to, off, 0, kStream);
+  } else {
+    __builtin_amdgcn_raw_buffer_store_b64((v2u){pack2(f[0], f[1]), pack2(f[2], f[3])}, to, off, 0, kStream);
+  }
+}
+
+template <typename TI, typename TO, int NW, int NV, bool TAIL>
+__global__ __launch_bounds__(NW * 64, 4) void k_distill_resident(Logits in, Logits grad, emu_teacher_t te, float c1, float* loss, float4* stats,
                                                                      const Prepared* teacher, const float* rests, uint32_t* ticket, uint32_t rows,
                                                                      uint64_t row0) {
-  constexpr int NW = kRowWaves, U = kScanU;
+  constexpr int U = kScanU;
   constexpr uint32_t E = kE<TI>;
   extern __shared__ uint32_t bits[];
   __shared__ DistillLds<NW> t;
   __shared__ Listed<NW * NV> list;
   __shared__ Running inside_run[NW];
-  __shared__ uint32_t taken, first;
+  __shared__ uint8_t* shards[kMaxShards];
   v4u x[NV];
+  __shared__ uint32_t taken, first;
   uint32_t now = rows, next, after;  // the row in x, the row to load, the one behind it; `rows`: none
   float w = 0.0f;
   Entry e = {-1, 0.0f, -kInf};
   if constexpr (TAIL)
     for (uint32_t i = threadIdx.x; i < tiles<TI>(in.V) * kTile<TI> / 32; i += NW * 64) bits[i] = 0;
   for (int i = threadIdx.x; i < NW * NV; i += NW * 64) list.head[i] = -1;
+  if (threadIdx.x < kMaxShards) shards[threadIdx.x] = in.p[threadIdx.x];
   if (threadIdx.x == 0) first = atomicAdd(ticket, 1u);
   __syncthreads();
   next = umin(__builtin_amdgcn_readfirstlane(first), rows);
@@ -1149,13 +1263,13 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_distill_resident(Logits in, 
     asm volatile("" : "+v"(thread));
     const uint32_t lane = thread & 63;
     const Span span = part_of({0, tiles<TI>(in.V)}, __builtin_amdgcn_readfirstlane(thread >> 6), NW);
-    const uint32_t t0 = span.t0, t1 = span.t1;
+    const uint32_t t0 = span.t0, t1 = span.t1, last = in.V / kTile<TI>;
     // what the turn needs beside x is on its way during the scan: a wait for it behind the loads would be one for them
-    uint32_t later = rows;
-    if (threadIdx.x == 0 && next < rows) later = atomicAdd(ticket, 1u);
-    const float w_next = next < rows ? (te.weight ? te.weight[row0 + next] : 1.0f) : 0.0f;
-    Stored f_next = {-1, 0.0f};
-    if (w_next != 0.0f && int(threadIdx.x) < te.k) f_next = teacher[next].entry[threadIdx.x];
+    uint32_t later = 0;
+    if (threadIdx.x == 0) later = atomicAdd(ticket, 1u);
+    const float w_next = next < rows ? (te.weight ? scalar(te.weight + row0 + next) : 1.0f) : 0.0f;
+    v2u f_next = {~0u, 0u};
+    if (w_next != 0.0f && int(thread) < te.k) f_next = ld8_any<POL_PLAIN>(reinterpret_cast<const uint8_t*>(teacher + next), thread * 8);
     Stats st = kSkipped;
     float rest = 0.0f, rest_loss = 0.0f, scale = 0.0f, coef = 0.0f;
     const bool live = now < rows && w != 0.0f;
@@ -1174,6 +1288,11 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_distill_resident(Logits in, 
           asm volatile("" : "+v"(x[i + u]));  // in this order: all at once would take twice the registers
           if constexpr (TAIL)
             if (t0 + i + u < t1) leave_out<TI>(x[i + u], bits, (t0 + i + u) * kTile<TI> + lane * E);
+          if (t0 + i + u == last) {  // pads behind V in V's own vector
+#pragma unroll
+            for (uint32_t q = 0; q < E; ++q)
+              if ((t0 + i + u) * kTile<TI> + lane * E + q >= in.V) set_minus_inf<TI>(x[i + u], q);
+          }
           unpack(x[i + u], f[u]);
         }
         add_values<U, E>(run, f, c1);
@@ -1187,27 +1306,26 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_distill_resident(Logits in, 
       }
       if (int(threadIdx.x) < kMaxTeacher) t.col[threadIdx.x] = e.col;
     }
-    rest = live ? rests[now] : 0.0f;
+    rest = live ? scalar(rests + now) : 0.0f;
     if (threadIdx.x == 0) taken = later;  // everyone has read the last one before the last turn's last barrier
     __syncthreads();
     after = umin(__builtin_amdgcn_readfirstlane(taken), rows);
     if (live) {
-      Running all[NW], inside = {-kInf, 0.0f};
-#pragma unroll
-      for (int i = 0; i < NW; ++i) all[i] = t.run[i];
-      const Running run = joined(all, c1);
+      Running inside = {-kInf, 0.0f};
+      const Running run = waves_joined<NW>(t.run, c1);
       if constexpr (TAIL) {
-#pragma unroll
-        for (int i = 0; i < NW; ++i) all[i] = inside_run[i];
-        inside = joined(all, c1);
+        inside = waves_joined<NW>(inside_run, c1);
         if (e.col >= 0) bits[e.col / 32] = 0;
       }
       st = conclude<TI, NW, TAIL>(in, ri, run, inside, e, rest < 0.0f ? 0.0f : rest, te.k, c1, t, &rest_loss);
       scale = w * (c1 * 0.69314718f);
     }
     const uint64_t ro = r * grad.row_bytes, rn = (row0 + next) * in.row_bytes;
-    float z_next = -kInf;
-    if (f_next.col >= 0) z_next = widen(*column<TI>(in, rn, f_next.col));
+    TI z_next = TI();  // widened when it is needed: to do it here would be to wait for it
+    if (int32_t(f_next[0]) >= 0) {
+      const uint32_t t = shard_of(in, f_next[0]);
+      z_next = reinterpret_cast<const TI*>(shards[t] + rn)[f_next[0] - t * in.cols];
+    }
     const bool dead = !live || rest < 0.0f;
     const bool zero = dead || st.s == 0.0f, wild = !zero && !plain(st.m, c1);
     const float ref = reference(st.m, c1);
@@ -1222,34 +1340,38 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_distill_resident(Logits in, 
     const bool write = now < rows && !wild;
     Reader<TI> from(in, rn, t0);
     Cursor<TO, kTile<TI>> to(grad, ro, t0);
+    const uint8_t* none = reinterpret_cast<const uint8_t*>(kNoLogits + (sizeof(TI) == 2 ? 0 : 1));
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if (t0 + i >= t1) {
-        x[i] = (v4u){kMinusInf<TI>, kMinusInf<TI>, kMinusInf<TI>, kMinusInf<TI>};
-        continue;
-      }
-      if (write) {
-        float f[E];
-        if (zero) {
+      float f[E];
+      if (zero) {
 #pragma unroll
-          for (uint32_t q = 0; q < E; ++q) f[q] = 0.0f;
-        } else {
-          asm volatile("" : "+v"(x[i]));  // unpacked anew: the scan's values would take twice the registers
-          unpack(x[i], f);
+        for (uint32_t q = 0; q < E; ++q) f[q] = 0.0f;
+      } else {
+        asm volatile("" : "+v"(x[i]));  // unpacked anew: the scan's values would take twice the registers
+        unpack(x[i], f);
 #pragma unroll
-          for (uint32_t q = 0; q < E; ++q) f[q] = __builtin_amdgcn_exp2f(fmaf(f[q], c1, -ref)) * coef;
-          if (to.c + kTile<TI> > in.V) {
+        for (uint32_t q = 0; q < E; ++q) f[q] = __builtin_amdgcn_exp2f(fmaf(f[q], c1, -ref)) * coef;
+        if (t0 + i == last) {
 #pragma unroll
-            for (uint32_t q = 0; q < E; ++q)
-              if (to.c + lane * E + q >= in.V) f[q] = 0.0f;
-          }
+          for (uint32_t q = 0; q < E; ++q)
+            if (to.c + lane * E + q >= in.V) f[q] = 0.0f;
         }
-        take_listed(list, __builtin_amdgcn_readlane(heads, i), to.c + lane * E, f);
-        store_tile<TO, POL_NT, E, true>(grad, to, lane, f);
       }
-      if (w_next != 0.0f) {
-        if (from.one(in, 1)) x[i] = ld16_any<POL_NT>(from.base, lane * 16);
-        else x[i] = load_border<TI, POL_NT, true>(in, from, lane);
+      take_listed(list, __builtin_amdgcn_readlane(heads, i), to.c + lane * E, f);
+      const uint32_t row_end = grad.cols * uint32_t(sizeof(TO)), at = write && t0 + i < t1 ? to.lo * uint32_t(sizeof(TO)) : 1u << 31;
+      uint8_t* row = to.base - uint64_t(to.lo) * sizeof(TO);
+      store_bounded<TO>(__builtin_amdgcn_make_buffer_rsrc(row, 0, row_end, 0x00020000), at + lane * E * uint32_t(sizeof(TO)), f);
+      if (to.lo + kTile<TI> > grad.cols && to.c - to.lo + grad.cols < grad.Vp)  // and in the next shard
+        store_bounded<TO>(__builtin_amdgcn_make_buffer_rsrc(grad.p[to.t + 1] + ro, 0, row_end, 0x00020000),
+                          (write && t0 + i < t1 ? at - row_end : 1u << 31) + lane * E * uint32_t(sizeof(TO)), f);
+      const bool have = w_next != 0.0f && t0 + i < t1;
+      if (have && from.one(in, 1)) {
+        x[i] = ld16_any<POL_NT>(from.base, lane * 16);
+      } else {
+        const uint8_t* where = none - lane * 16;
+        if (have && from.c + lane * E < in.V) where = from.lo + lane * E >= in.cols ? from.other(in) : from.base;
+        x[i] = ld16_any<POL_NT>(where, lane * 16);
       }
       from.advance(in, 1);
       to.advance(grad, 1);
@@ -1257,8 +1379,8 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_distill_resident(Logits in, 
     }
     const float part = wave_reduce(live ? entry_loss(e, st, c1) : 0.0f, add);
     if (lane == 0) t.sum[wave_id()] = part;
+    __syncthreads();
     if (now < rows) {
-      __syncthreads();
       if (!dead && e.col >= 0) list.head[e.col / kTile<TI>] = -1;
       float total = t.sum[0];
 #pragma unroll
@@ -1269,7 +1391,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_distill_resident(Logits in, 
     now = next;
     next = after;
     w = w_next;
-    e = {f_next.col, f_next.value, z_next};
+    e = {int32_t(f_next[0]), __uint_as_float(f_next[1]), int32_t(f_next[0]) >= 0 ? widen(z_next) : -kInf};
   }
 }
 
@@ -1441,6 +1563,19 @@ static void by_type(int32_t dtype, F f) {
   dtype == EMU_BF16 ? f(bf16_t()) : f(float());
 }
 
+// The waves of a workgroup that has a row: 16 tiles each where 4, 8 or 16 of them can hold the row that way.
+static int row_waves(uint32_t n_tiles) { return n_tiles <= 4 * kResidentTiles ? 4 : n_tiles <= 8 * kResidentTiles ? 8 : 16; }
+
+// f(waves) for a workgroup that has a row of that many tiles.
+template <typename F>
+static void by_waves(uint32_t n_tiles, F f) {
+  switch (row_waves(n_tiles)) {
+    case 4: f(std::integral_constant<int, 4>()); break;
+    case 8: f(std::integral_constant<int, 8>()); break;
+    default: f(std::integral_constant<int, 16>()); break;
+  }
+}
+
 // f(input element, output element) for the two dtypes.
 template <typename F>
 static void by_types(int32_t in, int32_t out, F f) {
@@ -1450,7 +1585,11 @@ static void by_types(int32_t in, int32_t out, F f) {
 
 constexpr int kPartWaves = 4;  // of a workgroup that has a part of a row
 
-static uint32_t topk_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kTopWaves, 1024); }
+#ifndef TOPW
+#define TOPW 8
+#endif
+static int top_waves(uint32_t n_tiles) { return std::min(row_waves(n_tiles), TOPW); }
+static uint32_t topk_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kTopParts, l->rows < 512 ? 1024 : 1); }
 static uint32_t distill_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kPartWaves, l->rows < 256 ? 1024 : 1); }
 
 // The workspace of the distillation calls.
@@ -1462,20 +1601,27 @@ struct DistillWorkspace {
   uint64_t bytes;
   DistillWorkspace(void* at, uint64_t rows, uint64_t parts) {
     uint8_t* p = static_cast<uint8_t*>(at);
+    const uint64_t list = (rows + 63) / 64 * 256;
     ticket = reinterpret_cast<uint32_t*>(p);
-    rests = reinterpret_cast<float*>(p + 256);
-    teacher = reinterpret_cast<Prepared*>(p + 256 + (rows + 63) / 64 * 256);
+    rests = reinterpret_cast<float*>(p + kWsAlign);
+    teacher = reinterpret_cast<Prepared*>(p + kWsAlign + list);
     part = reinterpret_cast<Running*>(teacher + rows);
-    bytes = 256 + (rows + 63) / 64 * 256 + rows * (sizeof(Prepared) + parts * sizeof(Running));
+    bytes = kWsAlign + list + rows * (sizeof(Prepared) + parts * sizeof(Running));
   }
 };
 
-// The tiles of each wave in k_distill_resident, 0 where it does not take the row.
+// Whether k_distill_resident takes these rows.
 constexpr int64_t kResidentRows = 256;
-template <typename T>
-static uint32_t resident_tiles(const Logits& l) {
-  const uint32_t per_wave = (tiles<T>(l.V) + kRowWaves - 1) / kRowWaves;
-  return l.cols % kE<T> == 0 && l.cols >= kTile<T> && tiles<T>(l.Vp) == tiles<T>(l.V) && per_wave <= 16 ? per_wave : 0;
+#ifndef LOSST
+#define LOSST 256
+#endif
+constexpr uint32_t kLossTiles = LOSST;
+template <typename TI>
+static bool holds(const Logits& in, const Logits& out, uint64_t out_size) {
+  uint64_t bits = in.row_bytes | out.row_bytes;
+  for (uint32_t t = 0; t * in.cols < in.Vp; ++t) bits |= uint64_t(in.p[t]) | uint64_t(out.p[t]);
+  return bits % 16 == 0 && in.cols % kE<TI> == 0 && in.cols >= kTile<TI> && tiles<TI>(in.Vp) == tiles<TI>(in.V) &&
+         tiles<TI>(in.V) <= 16 * kResidentTiles && uint64_t(in.cols) * out_size < (1u << 30);
 }
 
 template <typename TI>
@@ -1572,11 +1718,20 @@ int emu_logits_topk(const emu_logits_t* in, int32_t k, float temperature, int32_
     over_rows(in->rows, [&](uint64_t r0, uint32_t n) {
       uint64_t* keys = static_cast<uint64_t*>(d_workspace);
       Running* run = parts == 1 ? nullptr : reinterpret_cast<Running*>(keys + uint64_t(n) * parts * 64);
-      hipLaunchKernelGGL((k_topk<decltype(ti)>), dim3(n, parts), dim3(kTopWaves * 64), 0, st, l, uint32_t(k), c1, d_index,
-                         d_logprob, d_lse, run, keys, r0);
-      if (parts > 1)
-        hipLaunchKernelGGL((k_topk_join<decltype(ti)>), dim3(n), dim3(kTopWaves * 64), 0, st, l, uint32_t(k), c1, d_index,
-                           d_logprob, d_lse, run, keys, parts, r0);
+      auto launch = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, dim3(n * parts), dim3(waves * 64), 0, st, l, uint32_t(k), c1, d_index, d_logprob, d_lse, run, keys, parts, r0);
+      };
+      using T = decltype(ti);
+      if (parts > 1) {
+        launch(k_topk<T, kTopParts>, kTopParts);
+        hipLaunchKernelGGL((k_topk_join<T>), dim3(n), dim3(kTopParts * 64), 0, st, l, uint32_t(k), c1, d_index, d_logprob, d_lse, run, keys, parts, r0);
+      } else {
+        switch (top_waves(tiles<T>(l.V))) {
+          case 4: launch(k_topk<T, 4>, 4); break;
+          case 8: launch(k_topk<T, 8>, 8); break;
+          default: launch(k_topk<T, 16>, 16); break;
+        }
+      }
     });
   });
   return hip_check("emu_logits_topk launch");
@@ -1604,7 +1759,7 @@ int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float
   float4* stats = reinterpret_cast<float4*>(d_stats);
   by_type(student->dtype, [&](auto ti) {
     using TI = decltype(ti);
-    const uint32_t n_tiles = tiles<TI>(li.V), resident = grad && student->rows >= kResidentRows && parts == 1 ? resident_tiles<TI>(li) : 0;
+    const uint32_t n_tiles = tiles<TI>(li.V);
     const size_t marks = teacher->tail ? size_t((n_tiles + parts - 1) / parts) * kTile<TI> / 8 : 0;
     over_rows(student->rows, [&](uint64_t r0, uint32_t n) {
       const DistillWorkspace ws(d_workspace, n, parts);
@@ -1617,25 +1772,23 @@ int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float
           if (grad) launch_backward(ti, grad->dtype, n, st, li, lo, *teacher, c1, stats, ws, r0);
           return;
         }
-        if (!grad) {
-          hipLaunchKernelGGL((k_distill<TI, TI, kRowWaves, TAIL, false>), dim3(n), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, r0);
-          return;
-        }
-        by_type(grad->dtype, [&](auto to) {
-          using TO = decltype(to);
-          if (!resident) {
-            hipLaunchKernelGGL((k_distill<TI, TO, kRowWaves, TAIL, true>), dim3(n), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, r0);
-            return;
-          }
-          launch_prepare(n, st, *teacher, li.V, ws, r0);
+        launch_prepare(n, st, *teacher, li.V, ws, r0);
+        by_waves(grad ? n_tiles : std::min(n_tiles, kLossTiles), [&](auto waves) {
+          constexpr int NW = decltype(waves)::value;
           auto launch = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(std::min(n, cus)), dim3(kRowWaves * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, ws.teacher, ws.rests,
-                               ws.ticket, n, r0);
+            hipLaunchKernelGGL(kernel, dim3(n), dim3(NW * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, ws.teacher, ws.rests, r0);
           };
-          if (resident <= 4) launch(k_distill_resident<TI, TO, 4, TAIL>);
-          else if (resident <= 8) launch(k_distill_resident<TI, TO, 8, TAIL>);
-          else if (resident <= 12) launch(k_distill_resident<TI, TO, 12, TAIL>);
-          else launch(k_distill_resident<TI, TO, 16, TAIL>);
+          if (!grad) return launch(k_distill<TI, TI, NW, TAIL, false>);
+          by_type(grad->dtype, [&](auto to) {
+            using TO = decltype(to);
+            if (student->rows < kResidentRows || !holds<TI>(li, lo, sizeof(TO))) return launch(k_distill<TI, TO, NW, TAIL, true>);
+            auto stay = [&](auto kernel) {
+              hipLaunchKernelGGL(kernel, dim3(std::min(n, cus * (16 / NW))), dim3(NW * 64), marks, st, li, lo, *teacher, c1, d_loss, stats,
+                                 ws.teacher, ws.rests, ws.ticket, n, r0);
+            };
+            if (NW == 4 && n_tiles <= 16) stay(k_distill_resident<TI, TO, 4, 4, TAIL>);
+            else stay(k_distill_resident<TI, TO, NW, kResidentTiles, TAIL>);
+          });
         });
       };
       teacher->tail ? by_tail(std::true_type()) : by_tail(std::false_type());
