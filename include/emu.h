@@ -387,7 +387,7 @@ int emu_check_bucket_tables(emu_plan_t plan, int32_t side, uint64_t bucket_bytes
  *     call must not overlap (undefined behaviour).
  *   - Sums, softmax statistics and losses are fp32 or wider, rounded to the output's type once. No result
  *     depends on the order of atomics.
- *   - Limits: tp <= 64, Vp <= 2^20, rows <= 2^31 - 1, 2^28 tokens per row (EMU_ERR_UNSUPPORTED); zero rows are a call that does nothing.
+ *   - Limits: tp <= 64, Vp <= 2^20, rows <= 2^31 - 1, tokens_cols < 2^20 (EMU_ERR_UNSUPPORTED); zero rows are a call that does nothing.
  *   - A workspace (emu_logits_workspace) holds what the workgroups of one call hand each other. It needs no
  *     initial contents and keeps nothing for later calls. Two calls that may run at the same time need two. */
 

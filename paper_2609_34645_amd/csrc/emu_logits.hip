@@ -12,7 +12,7 @@ namespace emu {
 
 constexpr int kMaxShards = 64;
 constexpr int32_t kMaxVocab = 1 << 20;
-constexpr int32_t kMaxTokens = 1 << 28;  // of one row's history: byte offsets stay below 2^32
+constexpr int32_t kMaxTokens = (1 << 20) - 1;  // of one row's history
 constexpr int kMaxTop = 64;        // entries of emu_logits_topk: one per lane of a wave
 constexpr int kMaxTeacher = 256;   // entries of a teacher's row
 constexpr uint32_t kMaxSplits = 64;            // workgroups that share a row: one partial result per lane
@@ -391,155 +391,215 @@ __device__ __forceinline__ float log_prob(float x, float m, float s, float c1) {
 // ------------------------------------------------------------------------------------------------
 // constraints
 // ------------------------------------------------------------------------------------------------
-// A workgroup has kSlice columns of one row. It counts the slice's tokens in LDS (integer atomics: any order gives
-// the same counts), marks the columns that anything concerns in a bit each, and passes over its columns once: a
-// vector whose mark and mask bytes are plain is copied, one that the mask forbids whole is not read.
+// A workgroup has SLICE columns of one row. Its logits are on their way from the start (but for vectors that the mask
+// forbids whole, and in place, where most vectors stay as they are); meanwhile it goes over the row's history and
+// counts the slice's tokens in LDS (integer atomics: any order gives the same counts). The slice's biases lie in
+// LDS in list order, the first of a column with the sum of all of them. Then every vector is copied, masked or
+// changed once: a column's word says all that concerns it, 0 that nothing does.
 
-constexpr int kConstrainThreads = 256;
-constexpr uint32_t kSlice = 8192;
-constexpr uint32_t kSeen = 1u << 31, kBiased = 1u << 30, kCountBits = kBiased - 1;
-constexpr int kListed = 512;  // biases of a slice held in LDS, in list order
+constexpr uint32_t kSeen = 1u << 31, kCountBits = (1u << 20) - 1;
+constexpr uint32_t kSlotShift = 20, kSlotBits = 1023;  // of the column's first bias, from 1 on; kSlotBits: not in the list
+constexpr int kListed = 512;                           // biases of a slice held in LDS
+// Workgroups of 512 threads on 8,192 columns took 14.8 us for 64 rows of 128,256 with histories of 2,500 (256 threads 15.4);
+// 1,024 threads on 16,384 took 73 us for 256 rows with 20,480 (on 32,768 77, 512 threads 84).
+constexpr int32_t kLongHistory = 8192;
 
-template <typename TI, typename TO>
-__global__ __launch_bounds__(kConstrainThreads) void k_constrain(Logits in, Logits out, emu_constraints_t c, bool in_place,
-                                                                 uint64_t row0) {
-  __shared__ uint32_t count[kSlice];
-  __shared__ uint32_t mark[kSlice / 32];
+template <typename TI, typename TO, int NT, uint32_t SLICE>
+__global__ __launch_bounds__(NT) void k_constrain(Logits in, Logits out, emu_constraints_t c, bool in_place, uint32_t slices, uint64_t row0) {
+  __shared__ __align__(16) uint32_t count[SLICE];
   __shared__ int32_t list_col[kListed];
-  __shared__ float list_value[kListed];
-  __shared__ uint32_t wave_n[kConstrainThreads / 64];
-  constexpr int U = 4;
-  constexpr uint32_t E = kE<TI>, kChunk = U * kTile<TI>;
-  const uint64_t r = row0 + blockIdx.x;
-  const uint32_t c0 = blockIdx.y * kSlice, c1 = umin(c0 + kSlice, in.Vp), lane = threadIdx.x & 63;
+  __shared__ float list_value[kListed], total[kListed];
+  __shared__ uint32_t listed;
+  constexpr uint32_t E = kE<TI>, TILES = SLICE / (NT / 64) / kTile<TI>, kAll = (1u << E) - 1;  // tiles of a wave
+  const uint32_t row = blockIdx.x / slices, c0 = (blockIdx.x - row * slices) * SLICE, c1 = umin(c0 + SLICE, in.Vp);
+  const uint64_t r = row0 + row, ri = r * in.row_bytes, ro = r * out.row_bytes;
+  const uint32_t lane = threadIdx.x & 63, first = c0 / kTile<TI> + wave_id() * TILES;
+  const uint8_t* mask = nullptr;
+  if (c.mask) {
+    const int64_t which = c.mask_row ? int64_t(scalar(c.mask_row + r)) : int64_t(r);
+    if (which >= 0 && which < c.n_masks) mask = reinterpret_cast<const uint8_t*>(c.mask + which * c.mask_stride);
+  }
+  uint32_t allowed[TILES];
+  v4u x[TILES];
+#pragma unroll
+  for (uint32_t u = 0; u < TILES; ++u) {
+    const uint32_t v = (first + u) * kTile<TI> + lane * E;
+    allowed[u] = kAll;
+    if (mask && v < in.V) allowed[u] = mask[v / 8];
+  }
+#pragma unroll
+  for (uint32_t u = 0; u < TILES; ++u) {
+    const uint32_t v = (first + u) * kTile<TI> + lane * E;
+    if (mask && v < in.V) allowed[u] = (allowed[u] >> (v % 8)) & kAll;
+  }
+  auto load = [&](uint32_t u, Reader<TI>& at, bool wanted) {
+    x[u] = (v4u){kMinusInf<TI>, kMinusInf<TI>, kMinusInf<TI>, kMinusInf<TI>};
+    if (at.c < in.V && wanted) {
+      if (at.one(in, 1)) x[u] = ld16_any<POL_NT>(at.base, lane * 16);
+      else x[u] = load_border<TI, POL_NT>(in, at, lane);
+    }
+    at.advance(in, 1);
+  };
+  if (!in_place) {
+    Reader<TI> at(in, ri, first);
+#pragma unroll
+    for (uint32_t u = 0; u < TILES; ++u) load(u, at, allowed[u] != 0);
+  }
+
   const bool concerns = c.tokens || c.bias_first;
   int64_t b0 = 0, b1 = 0;
-  uint32_t n_listed = 0;
   if (concerns) {
-    for (uint32_t i = threadIdx.x * 4; i < kSlice; i += kConstrainThreads * 4) *reinterpret_cast<v4u*>(count + i) = (v4u){0, 0, 0, 0};
-    for (uint32_t i = threadIdx.x; i < kSlice / 32; i += kConstrainThreads) mark[i] = 0;
+    for (uint32_t i = threadIdx.x * 4; i < SLICE; i += NT * 4) *reinterpret_cast<v4u*>(count + i) = (v4u){0, 0, 0, 0};
+    if (threadIdx.x == 0) listed = 0;
     __syncthreads();
+  }
+  const uint32_t own = umin(in.V - umin(c0, in.V), SLICE);  // the slice's columns below V
+  if (c.bias_first) {
+    b0 = min(max(int64_t(scalar(c.bias_first + r)), int64_t(0)), c.n_bias);
+    b1 = min(max(int64_t(scalar(c.bias_first + r + 1)), int64_t(0)), c.n_bias);
+    if (wave_id() == NT / 64 - 1) {  // the last wave, while the others are in the history
+      uint32_t n = 0;
+      for (int64_t i0 = b0 + lane; i0 - lane < b1; i0 += 256) {
+        uint32_t at[4];
+        float value[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) at[q] = (i0 + q * 64 < b1 ? uint32_t(c.bias_token[i0 + q * 64]) : ~0u) - c0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) value[q] = i0 + q * 64 < b1 ? c.bias_value[i0 + q * 64] : 0.0f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bool here = i0 + q * 64 < b1 && at[q] < own;
+          const uint64_t lanes = __ballot(here);
+          const uint32_t pos = n + __popcll(lanes & ((1ull << lane) - 1));
+          if (here && pos < kListed) {
+            list_col[pos] = int32_t(at[q] + c0);
+            list_value[pos] = value[q];
+          }
+          n += __popcll(lanes);
+        }
+      }
+      if (lane == 0) listed = n;
+    }
   }
   if (c.tokens) {
     const int32_t* tok = c.tokens + r * c.tokens_stride;
-    const int32_t n = min(max(c.seq_len[r], 0), c.tokens_cols);
-    const int32_t prompt = c.prompt_len ? c.prompt_len[r] : 0;
+    const int32_t n = min(max(scalar(c.seq_len + r), 0), c.tokens_cols);
+    const int32_t prompt = c.prompt_len ? scalar(c.prompt_len + r) : 0;
     auto take = [&](uint32_t v, int32_t i) {
       const uint32_t at = v - c0;
-      if (at < kSlice && v < in.V) {
-        if (i >= prompt) atomicAdd(&count[at], 1u);
-        atomicOr(&count[at], kSeen);
-        atomicOr(&mark[at / 32], 1u << (at % 32));
+      if (at < own) {
+        if (i < prompt) atomicOr(&count[at], kSeen);
+        else atomicAdd(&count[at], 1u);
       }
     };
+    // four vectors a thread in flight; behind the last whole one, token by token
+    constexpr int32_t kStep = NT * 4;
     const int32_t whole = n & ~3;
-    for (int32_t i = threadIdx.x * 4; i < whole; i += kConstrainThreads * 4) {
-      const v4u v = ld16_any<POL_PLAIN>(reinterpret_cast<const uint8_t*>(tok), uint32_t(i) * 4);
+    for (int32_t i0 = threadIdx.x * 4; i0 < whole; i0 += 4 * kStep) {
+      v4u v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) take(v[e], i + e);
+      for (int q = 0; q < 4; ++q)
+        v[q] = i0 + q * kStep < whole ? ld16_any<POL_PLAIN>(reinterpret_cast<const uint8_t*>(tok), uint32_t(i0 + q * kStep) * 4) : (v4u){~0u, ~0u, ~0u, ~0u};
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) take(v[q][e], i0 + q * kStep + e);
     }
     if (int32_t(threadIdx.x) < n - whole) take(uint32_t(tok[whole + threadIdx.x]), whole + threadIdx.x);
   }
-  if (c.bias_first) {
-    b0 = min(max(int64_t(c.bias_first[r]), int64_t(0)), c.n_bias);
-    b1 = min(max(int64_t(c.bias_first[r + 1]), int64_t(0)), c.n_bias);
-    for (int64_t i0 = b0; i0 < b1; i0 += kConstrainThreads) {
-      const int64_t i = i0 + threadIdx.x;
-      const uint32_t v = i < b1 ? uint32_t(c.bias_token[i]) : ~0u, at = v - c0;
-      const bool here = at < kSlice && v < in.V;
-      const uint64_t lanes = __ballot(here);
-      if (lane == 0) wave_n[threadIdx.x >> 6] = __popcll(lanes);
-      __syncthreads();
-      uint32_t pos = n_listed + __popcll(lanes & ((1ull << lane) - 1));
-#pragma unroll
-      for (uint32_t w = 0; w < kConstrainThreads / 64; ++w) {
-        if (w < (threadIdx.x >> 6)) pos += wave_n[w];
-        n_listed += wave_n[w];
-      }
-      if (here) {
-        if (pos < kListed) {
-          list_col[pos] = int32_t(v);
-          list_value[pos] = c.bias_value[i];
-        }
-        atomicOr(&count[at], kBiased);
-        atomicOr(&mark[at / 32], 1u << (at % 32));
-      }
-      __syncthreads();
-    }
-  }
   __syncthreads();
-  const uint8_t* mask = nullptr;
-  if (c.mask) {
-    const int64_t which = c.mask_row ? int64_t(c.mask_row[r]) : int64_t(r);
-    if (which >= 0 && which < c.n_masks) mask = reinterpret_cast<const uint8_t*>(c.mask + which * c.mask_stride);
+  if (c.bias_first) {
+    const uint32_t n = listed;
+    if (n <= kListed) {
+      for (uint32_t j = threadIdx.x; j < n; j += NT) {
+        const int32_t col = list_col[j];
+        float sum = 0.0f;
+        bool leads = true;
+        for (uint32_t i = 0; i < n; ++i) {
+          if (list_col[i] != col) continue;
+          leads &= i >= j;
+          sum += list_value[i];
+        }
+        if (leads) {
+          total[j] = sum;
+          atomicOr(&count[col - c0], (j + 1) << kSlotShift);
+        }
+      }
+    } else {
+      for (int64_t i = b0 + threadIdx.x; i < b1; i += NT) {
+        const uint32_t at = uint32_t(c.bias_token[i]) - c0;
+        if (at < own) atomicOr(&count[at], kSlotBits << kSlotShift);
+      }
+    }
+    __syncthreads();
   }
-  const float theta = c.repetition ? c.repetition[r] : 1.0f;
-  const float af = c.frequency ? c.frequency[r] : 0.0f, ap = c.presence ? c.presence[r] : 0.0f;
-  auto concerned = [&](float x, uint32_t v) {
-    const uint32_t n = count[v - c0];
-    if (n & kSeen) {
-      x = x > 0.0f ? x / theta : x * theta;
-      if (n & kCountBits) x -= af * float(n & kCountBits) + ap;
-    }
-    if (n & kBiased) {
-      float sum = 0.0f;
-      if (n_listed <= kListed) {
-        for (uint32_t i = 0; i < n_listed; ++i)
-          if (list_col[i] == int32_t(v)) sum += list_value[i];
-      } else {
-        for (int64_t i = b0; i < b1; ++i)
-          if (c.bias_token[i] == int32_t(v)) sum += c.bias_value[i];
-      }
-      x += sum;
-    }
-    return x;
+
+  // x / theta as a product with the rounded 1 / theta: off by half a step more than a division, at a tenth of its price
+  const float theta = c.repetition ? scalar(c.repetition + r) : 1.0f, inverse = 1.0f / theta;
+  const float af = c.frequency ? scalar(c.frequency + r) : 0.0f, ap = c.presence ? scalar(c.presence + r) : 0.0f;
+  auto bias = [&](uint32_t slot, uint32_t v) {
+    if (slot != kSlotBits) return total[slot - 1];
+    float sum = 0.0f;
+    for (int64_t i = b0; i < b1; ++i)
+      if (c.bias_token[i] == int32_t(v)) sum += c.bias_value[i];
+    return sum;
   };
-  constexpr uint32_t kAll = (1u << E) - 1;
-  const uint64_t ri = r * in.row_bytes, ro = r * out.row_bytes;
-  for (uint32_t cc = c0 + wave_id() * kChunk; cc < c1; cc += kConstrainThreads / 64 * kChunk) {
-    uint32_t allowed[U], marked[U];
-    bool kept[U];  // in place and unchanged
-    v4u x[U];
+  // what concerns a vector's columns, and whether anything does
+  auto words = [&](uint32_t u, uint32_t (&n)[E]) {
+    uint32_t any = 0;
+    const uint32_t at = (first + u) * kTile<TI> + lane * E - c0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t v = cc + u * kTile<TI> + lane * E;
-      allowed[u] = kAll;
-      if (mask && v < in.V) allowed[u] = (mask[v / 8] >> (v % 8)) & kAll;
-      marked[u] = concerns ? (reinterpret_cast<const uint8_t*>(mark)[(v - c0) / 8] >> (v % 8)) & kAll : 0;
-      kept[u] = in_place && !marked[u] && allowed[u] == kAll && v + E <= in.V;
-    }
-    const uint32_t t = shard_of(in, cc), lo = cc - t * in.cols;
-    const bool inside = lo + kChunk <= in.cols && cc + kChunk <= in.V;
-    const uint8_t* bi = in.p[t] + ri + uint64_t(lo) * sizeof(TI);
-    uint8_t* bo = out.p[t] + ro + uint64_t(lo) * sizeof(TO);
+    for (uint32_t q = 0; q < E; q += 4) {
+      const v4u four = concerns ? *reinterpret_cast<const v4u*>(count + at + q) : (v4u){0, 0, 0, 0};
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      x[u] = (v4u){kMinusInf<TI>, kMinusInf<TI>, kMinusInf<TI>, kMinusInf<TI>};
-      if (allowed[u] && !kept[u]) {
-        if (inside) x[u] = ld16_any<POL_NT>(bi, lane * 16 + u * 1024);
-        else x[u] = load_edge<TI, POL_NT>(in, ri, cc + u * kTile<TI> + lane * E);
+      for (uint32_t e = 0; e < 4; ++e) {
+        n[q + e] = four[e];
+        any |= four[e];
       }
     }
+    return any;
+  };
+  // in place, a vector stays where nothing concerns or forbids it and no pad ends it
+  auto kept = [&](uint32_t u, uint32_t any) { return in_place && !any && allowed[u] == kAll && (first + u) * kTile<TI> + lane * E + E <= in.V; };
+  if (in_place) {
+    Reader<TI> at(in, ri, first);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t v = cc + u * kTile<TI> + lane * E;
-      float f[E];
-      unpack(x[u], f);
-      const uint32_t touched = marked[u] & allowed[u];
-      if (touched) {
-#pragma unroll
-        for (uint32_t e = 0; e < E; ++e)
-          if ((touched >> e) & 1u) f[e] = concerned(f[e], v + e);
-      }
-      if (allowed[u] != kAll) {
-#pragma unroll
-        for (uint32_t e = 0; e < E; ++e)
-          if (!((allowed[u] >> e) & 1u)) f[e] = -kInf;
-      }
-      if (kept[u]) continue;
-      if (inside) store_values<TO, POL_NT>(bo, (lane * E + u * kTile<TI>) * uint32_t(sizeof(TO)), f);
-      else if (v < c1) store_edge<TO, POL_NT>(out, ro, v, f);
+    for (uint32_t u = 0; u < TILES; ++u) {
+      uint32_t n[E];
+      load(u, at, allowed[u] != 0 && !kept(u, words(u, n)));
     }
+  }
+  Cursor<TO, kTile<TI>> to(out, ro, first);
+#pragma unroll
+  for (uint32_t u = 0; u < TILES; ++u) {
+    const uint32_t v = (first + u) * kTile<TI> + lane * E;
+    if (to.c >= c1) break;
+    float f[E];
+    unpack(x[u], f);
+    uint32_t n[E];
+    const uint32_t any = words(u, n);
+    if (any && allowed[u]) {
+#pragma unroll
+      for (uint32_t e = 0; e < E; ++e) {  // without branches: * 1 and - 0 where nothing concerns the column
+        const uint32_t times = n[e] & kCountBits;
+        const float factor = n[e] & (kSeen | kCountBits) ? (f[e] > 0.0f ? inverse : theta) : 1.0f;
+        f[e] = f[e] * factor - (times ? fmaf(af, float(times), ap) : 0.0f);
+      }
+      if ((any >> kSlotShift) & kSlotBits) {
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e) {
+          const uint32_t slot = (n[e] >> kSlotShift) & kSlotBits;
+          if (slot) f[e] += bias(slot, v + e);
+        }
+      }
+    }
+    if (allowed[u] != kAll) {
+#pragma unroll
+      for (uint32_t e = 0; e < E; ++e)
+        if (!((allowed[u] >> e) & 1u)) f[e] = -kInf;
+    }
+    if (!kept(u, any)) store_tile<TO, POL_NT>(out, to, lane, f);
+    to.advance(out, 1);
   }
 }
 
@@ -1174,7 +1234,7 @@ __global__ __launch_bounds__(kPrepareWaves * 64) void k_prepare_teacher(emu_teac
   if (lane == 0) rest[row] = te.tail ? (left < 0.0f ? 0.0f : left) : sum == 0.0 ? -1.0f : 0.0f;
 }
 
-// One workgroup per row.
+// One workgroup per row. teacher NULL: entries as the caller stored them (few rows: a launch less).
 template <typename TI, typename TO, int NW, bool TAIL, bool GRAD>
 __global__ __launch_bounds__(NW * 64) void k_distill(Logits in, Logits grad, emu_teacher_t te, float c1, float* loss, float4* stats,
                                                      const Prepared* teacher, const float* rests, uint64_t row0) {
@@ -1190,14 +1250,21 @@ __global__ __launch_bounds__(NW * 64) void k_distill(Logits in, Logits grad, emu
     for (int i = threadIdx.x; i < kRowTiles; i += NW * 64) list.head[i] = -1;
   if (w != 0.0f) {
     Stored f = {-1, 0.0f};
-    if (int(threadIdx.x) < te.k) f = teacher[blockIdx.x].entry[threadIdx.x];
+    if (!teacher) f = fetch_teacher(te, r, in.V);
+    else if (int(threadIdx.x) < te.k) f = teacher[blockIdx.x].entry[threadIdx.x];
     const Span row = {0, tiles<TI>(in.V)};
     if constexpr (TAIL) mark_listed<NW>(bits, 0, row.t1 * kTile<TI>, f.col);
     const Running run = block_joined<NW>(scan<TI, NW, TAIL, GRAD ? POL_PLAIN : POL_NT>(in, off, row, c1, bits), t.run, c1);
-    e = {f.col, f.value, -kInf};
-    if (e.col >= 0) e.z = widen(*column<TI>(in, off, e.col));
-    if (int(threadIdx.x) < kMaxTeacher) t.col[threadIdx.x] = e.col;
-    rest = rests[blockIdx.x];
+    if (!teacher) {
+      bool none;
+      e = take_teacher<TI, NW>(t, f, te, r, in, 0, in.V, &rest, &none);
+      if (none) rest = -1.0f;
+    } else {
+      e = {f.col, f.value, -kInf};
+      if (e.col >= 0) e.z = widen(*column<TI>(in, off, e.col));
+      if (int(threadIdx.x) < kMaxTeacher) t.col[threadIdx.x] = e.col;
+      rest = rests[blockIdx.x];
+    }
     float value;
     st = finish<TI, NW, TAIL>(in, off, run, e, rest < 0.0f ? 0.0f : rest, te.k, c1, t, &value);
     write_row(loss, stats, r, value * w, st);
@@ -1585,10 +1652,8 @@ static void by_types(int32_t in, int32_t out, F f) {
 
 constexpr int kPartWaves = 4;  // of a workgroup that has a part of a row
 
-#ifndef TOPW
-#define TOPW 8
-#endif
-static int top_waves(uint32_t n_tiles) { return std::min(row_waves(n_tiles), TOPW); }
+// 4,096 rows of 128,256: 4 / 8 / 16 waves 224 / 210 / 280 us
+static int top_waves(uint32_t n_tiles) { return std::min(row_waves(n_tiles), 8); }
 static uint32_t topk_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kTopParts, l->rows < 512 ? 1024 : 1); }
 static uint32_t distill_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kPartWaves, l->rows < 256 ? 1024 : 1); }
 
@@ -1690,10 +1755,15 @@ int emu_logits_constrain(const emu_logits_t* in, const emu_logits_t* out, const 
   const bool in_place = out->shards[0] == in->shards[0];
   drop_pending_error();
   by_types(in->dtype, out->dtype, [&](auto ti, auto to) {
-    over_rows(in->rows, [&](uint64_t r0, uint32_t n) {
-      hipLaunchKernelGGL((k_constrain<decltype(ti), decltype(to)>), dim3(n, (li.Vp + kSlice - 1) / kSlice),
-                         dim3(kConstrainThreads), 0, st, li, lo, *c, in_place, r0);
-    });
+    auto launch = [&](auto kernel, uint32_t slice, int threads) {
+      const uint32_t slices = (li.Vp + slice - 1) / slice;
+      over_rows(in->rows, [&](uint64_t r0, uint32_t n) {
+        hipLaunchKernelGGL(kernel, dim3(n * slices), dim3(threads), 0, st, li, lo, *c, in_place, slices, r0);
+      });
+    };
+    // long histories: larger slices, so that fewer workgroups go over them
+    if (c->tokens && c->tokens_cols > kLongHistory) launch(k_constrain<decltype(ti), decltype(to), 1024, 16384>, 16384, 1024);
+    else launch(k_constrain<decltype(ti), decltype(to), 512, 8192>, 8192, 512);
   });
   return hip_check("emu_logits_constrain launch");
 }
@@ -1728,8 +1798,7 @@ int emu_logits_topk(const emu_logits_t* in, int32_t k, float temperature, int32_
       } else {
         switch (top_waves(tiles<T>(l.V))) {
           case 4: launch(k_topk<T, 4>, 4); break;
-          case 8: launch(k_topk<T, 8>, 8); break;
-          default: launch(k_topk<T, 16>, 16); break;
+          default: launch(k_topk<T, 8>, 8); break;
         }
       }
     });
@@ -1772,16 +1841,18 @@ int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float
           if (grad) launch_backward(ti, grad->dtype, n, st, li, lo, *teacher, c1, stats, ws, r0);
           return;
         }
-        launch_prepare(n, st, *teacher, li.V, ws, r0);
-        by_waves(grad ? n_tiles : std::min(n_tiles, kLossTiles), [&](auto waves) {
+        const bool prepared = student->rows >= kResidentRows;
+        if (prepared) launch_prepare(n, st, *teacher, li.V, ws, r0);
+        by_waves(n_tiles, [&](auto waves) {
           constexpr int NW = decltype(waves)::value;
           auto launch = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3(n), dim3(NW * 64), marks, st, li, lo, *teacher, c1, d_loss, stats, ws.teacher, ws.rests, r0);
+            hipLaunchKernelGGL(kernel, dim3(n), dim3(NW * 64), marks, st, li, lo, *teacher, c1, d_loss, stats,
+                               prepared ? ws.teacher : nullptr, ws.rests, r0);
           };
           if (!grad) return launch(k_distill<TI, TI, NW, TAIL, false>);
           by_type(grad->dtype, [&](auto to) {
             using TO = decltype(to);
-            if (student->rows < kResidentRows || !holds<TI>(li, lo, sizeof(TO))) return launch(k_distill<TI, TO, NW, TAIL, true>);
+            if (!prepared || !holds<TI>(li, lo, sizeof(TO))) return launch(k_distill<TI, TO, NW, TAIL, true>);
             auto stay = [&](auto kernel) {
               hipLaunchKernelGGL(kernel, dim3(std::min(n, cus * (16 / NW))), dim3(NW * 64), marks, st, li, lo, *teacher, c1, d_loss, stats,
                                  ws.teacher, ws.rests, ws.ticket, n, r0);

@@ -663,13 +663,13 @@ def shard_columns(layout: Layout) -> int:
 
 
 def _head(layout):
-    """(C layout, columns per shard), kept with the layout, which never changes."""
+    """(C layout, columns per shard, workspace sizes), kept with the layout, which never changes."""
     head = layout.__dict__.get("_head")
     if head is None:
         c = layout.c()
         check(load().emu_layout_check(ctypes.byref(c)))
         q = layout.tp * layout.pad
-        head = (c, (-(-layout.model.vocab // q) * q if q else layout.model.vocab) // layout.tp)
+        head = (ctypes.pointer(c), (-(-layout.model.vocab // q) * q if q else layout.model.vocab) // layout.tp, {})
         object.__setattr__(layout, "_head", head)
     return head
 
@@ -680,7 +680,7 @@ class LogitShards:
     shards have one dtype and one row stride."""
 
     def __init__(self, layout: Layout, tensors):
-        c, cols = _head(layout)
+        c, cols, self._sizes = layout.__dict__.get("_head") or _head(layout)
         tensors = list(tensors)
         if len(tensors) != layout.tp:
             raise ValueError(f"{len(tensors)} shards, the layout has tp={layout.tp}")
@@ -691,17 +691,21 @@ class LogitShards:
         code = BF16 if dtype is _bfloat16 else FP32 if dtype is _float32 else None
         if code is None:
             raise ValueError(f"logits must be bfloat16 or float32, not {dtype}")
-        rows = shape[0]
-        stride = first.stride(0) if rows > 1 else max(cols, first.stride(0))
+        rows, strides = shape[0], first.stride()
         for t in tensors:
-            if t.shape != shape or t.dtype is not dtype or (rows > 1 and t.stride(0) != stride):
+            if t is not first and (t.shape != shape or t.dtype is not dtype or (t.stride() != strides and rows > 1)):
                 raise ValueError("shards must have one shape, dtype and row stride")
             if cols > 1 and t.stride(1) != 1:
                 raise ValueError("the elements of a row must be adjacent")
-        _on_device(*tensors)
+        self.device = first.get_device()
+        if self.device < 0 or self.device != _device():
+            _misplaced(first, "a shard")
+        for t in tensors:
+            if t.get_device() != self.device:
+                _misplaced(t, "a shard")
         self.layout, self.tensors, self.rows, self.dtype = layout, tensors, rows, dtype
         self._ptrs = (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
-        self._c = c_logits(ctypes.pointer(c), code, len(tensors), rows, stride, self._ptrs)
+        self._c = c_logits(c, code, len(tensors), rows, max(cols, strides[0]) if rows == 1 else strides[0], self._ptrs)
         self.ref = ctypes.addressof(self._c)
 
     @classmethod
@@ -714,37 +718,55 @@ class LogitShards:
 
     def workspace(self, k: int = 0, stream=None):
         """(tensor or None, bytes) of a workspace for ``top_logprobs`` (k >= 1) or the distillation calls (k = 0)."""
-        n = ctypes.c_uint64()
-        check(load().emu_logits_workspace(self.ref, k, ctypes.addressof(n)))
-        return (_empty((n.value,), _uint8(), self.tensors[0], stream) if n.value else None), n.value
+        key = (self.rows, self.dtype, k)
+        size = self._sizes.get(key)
+        if size is None:
+            n = ctypes.c_uint64()
+            check(load().emu_logits_workspace(self.ref, k, ctypes.addressof(n)))
+            if len(self._sizes) > 256:
+                self._sizes.clear()
+            size = self._sizes[key] = n.value
+        return (_empty((size,), _uint8(), self.tensors[0], stream) if size else None), size
 
 
-def _on_device(*tensors):
-    """Every tensor on the current device: the calls launch there."""
-    for t in tensors:
-        if t is not None and not t.is_cuda:
-            raise ValueError("not a device tensor")
-    current = _current_device() if _current_device is not None else None
-    for t in tensors:
-        if t is not None and current is not None and t.get_device() != current:
-            raise ValueError(f"a tensor on device {t.get_device()}, the current device is {current}")
+def _device():
+    """The current device: the calls launch there."""
+    return _current_device() if _current_device is not None else 0
 
 
-def _operand(t, name, dtype, *shape):
-    """The address of an optional operand of the given type; a None in shape: any size. Rows may be strided."""
+def _misplaced(t, name):
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not a device tensor")
+    raise ValueError(f"{name} is on device {t.get_device()}, the current device is {_device()}")
+
+
+def _operand(t, name, dtype, shape, device):
+    """The address of an optional operand of the given type and shape, whole rows adjacent."""
     if t is None:
         return None
     if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{name} has shape {list(t.shape)}, expected {['*' if n is None else n for n in shape]}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {list(t.shape)}, expected {list(shape)}")
+    if not t.is_contiguous():
         raise ValueError(f"{name}: elements must be adjacent")
+    if t.get_device() != device:
+        _misplaced(t, name)
     return t.data_ptr()
 
 
-def _row_stride(t):
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _rows_operand(t, name, dtype, rows, cols, device):
+    """The same for a matrix whose rows may be strided; cols None: any number. (address, row stride)"""
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        raise ValueError(f"{name} has shape {list(shape)}, expected [{'*' if rows is None else rows}, {'*' if cols is None else cols}]")
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    if t.get_device() != device:
+        _misplaced(t, name)
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
 
 
 def _empty(shape, dtype, like, stream):
@@ -764,40 +786,41 @@ def constrain_logits(logits: LogitShards, out: LogitShards = None, tokens=None, 
     place). tokens int32 [rows, capacity] with seq_len int32 [rows] and optionally prompt_len int32 [rows]; repetition,
     frequency, presence fp32 [rows]; bias = (first int32 [rows + 1], token int32 [n], value fp32 [n]); mask
     int32 [n, words], one per row or chosen by mask_row int32 [rows] (negative: none)."""
-    rows, i32, f32 = logits.rows, _int32, _float32
+    rows, dev, i32, f32 = logits.rows, logits.device, _int32, _float32
     out = logits if out is None else out
-    c = c_constraints()
+    per_row = (rows,)
+    tok = tok_stride = tok_cols = length = prompt = 0
     if tokens is not None:
-        c.tokens = _operand(tokens, "tokens", i32, rows, None)
-        c.tokens_cols, c.tokens_stride = tokens.shape[1], _row_stride(tokens)
-        c.seq_len = _operand(seq_len, "seq_len", i32, rows)
-        c.prompt_len = _operand(prompt_len, "prompt_len", i32, rows)
-        if tokens.shape[1] == 0:
-            c.tokens = None
+        if seq_len is None:
+            raise ValueError("tokens without seq_len")
+        tok, tok_stride = _rows_operand(tokens, "tokens", i32, rows, None, dev)
+        tok_cols = tokens.shape[1]
+        length = _operand(seq_len, "seq_len", i32, per_row, dev)
+        prompt = _operand(prompt_len, "prompt_len", i32, per_row, dev)
     elif seq_len is not None or prompt_len is not None:
         raise ValueError("lengths without tokens")
-    c.repetition = _operand(repetition, "repetition", f32, rows)
-    c.frequency = _operand(frequency, "frequency", f32, rows)
-    c.presence = _operand(presence, "presence", f32, rows)
-    first = token = value = None
+    first = token = value = n_bias = 0
     if bias is not None:
         first, token, value = bias
-        n = c.n_bias = token.shape[0]
-        c.bias_first = _operand(first, "bias first", i32, rows + 1)
-        c.bias_token, c.bias_value = _operand(token, "bias token", i32, n), _operand(value, "bias value", f32, n)
-        if n == 0:
-            c.bias_first = None
+        listed = token.shape
+        if len(listed) != 1:
+            raise ValueError("bias token must be a vector")
+        n_bias = listed[0]
+        first = _operand(first, "bias first", i32, (rows + 1,), dev)
+        token, value = _operand(token, "bias token", i32, listed, dev), _operand(value, "bias value", f32, listed, dev)
+    allowed = mask_stride = n_masks = 0
     if mask is not None:
-        c.mask = _operand(mask, "mask", i32, None if mask_row is not None else rows, None)
-        c.n_masks, c.mask_stride = mask.shape[0], _row_stride(mask)
-        c.mask_row = _operand(mask_row, "mask_row", i32, rows)
-        if mask.shape[1] * 32 < logits.layout.model.vocab:
-            raise ValueError(f"mask rows of {mask.shape[1]} words are short of {logits.layout.model.vocab} tokens")
-        if mask.shape[0] == 0:
-            c.mask = None
+        allowed, mask_stride = _rows_operand(mask, "mask", i32, None if mask_row is not None else rows, None, dev)
+        n_masks, words = mask.shape
+        if words * 32 < logits.layout.model.vocab:
+            raise ValueError(f"mask rows of {words} words are short of {logits.layout.model.vocab} tokens")
     elif mask_row is not None:
         raise ValueError("mask_row without mask")
-    _on_device(tokens, seq_len, prompt_len, repetition, frequency, presence, first, token, value, mask, mask_row)
+    c = c_constraints(tok if tok_cols else 0, tok_stride, tok_cols, n_masks, length, prompt,
+                      _operand(repetition, "repetition", f32, per_row, dev),
+                      _operand(frequency, "frequency", f32, per_row, dev), _operand(presence, "presence", f32, per_row, dev),
+                      first if n_bias else 0, token, value, n_bias, allowed if n_masks else 0, mask_stride,
+                      _operand(mask_row, "mask_row", i32, per_row, dev))
     check(load().emu_logits_constrain(logits.ref, out.ref, ctypes.addressof(c), _stream_handle(stream)))
     return out
 
@@ -816,12 +839,10 @@ def top_logprobs(logits: LogitShards, k: int, temperature: float = 1.0, stream=N
 
 
 def _teacher(logits, index, value, weight, name, temperature, tail):
-    rows, k = logits.rows, index.shape[-1]
-    c = c_teacher(k, 1 if tail else 0, temperature, _operand(index, "index", _int32, rows, k), _row_stride(index),
-                  _operand(value, "teacher", _float32, rows, k), _row_stride(value),
-                  _operand(weight, name, _float32, rows))
-    _on_device(index, value, weight)
-    return c
+    rows, k, dev = logits.rows, index.shape[-1], logits.device
+    at, stride = _rows_operand(index, "index", _int32, rows, k, dev)
+    values, value_stride = _rows_operand(value, "teacher", _float32, rows, k, dev)
+    return c_teacher(k, 1 if tail else 0, temperature, at, stride, values, value_stride, _operand(weight, name, _float32, (rows,), dev))
 
 
 def distill_loss(logits: LogitShards, index, teacher, weight=None, temperature: float = 1.0, tail: bool = False,
@@ -845,10 +866,7 @@ def distill_backward(logits: LogitShards, index, teacher, stats, grad_loss, grad
     """``emu_distill_backward``: the gradient with respect to the logits, from the statistics of ``distill_loss`` and the
     gradient grad_loss fp32 [rows] of every row's unweighted loss, into ``grad`` (which may be the logits)."""
     c = _teacher(logits, index, teacher, grad_loss, "grad_loss", temperature, tail)
-    stats_ptr = _operand(stats, "stats", _float32, logits.rows, 4)
-    if logits.rows > 1 and stats.stride(0) != 4:
-        raise ValueError("stats must be contiguous")
-    _on_device(stats)
+    stats_ptr = _operand(stats, "stats", _float32, (logits.rows, 4), logits.device)
     ws, n = logits.workspace(0, stream)
     check(load().emu_distill_backward(logits.ref, ctypes.addressof(c), stats_ptr, grad.ref,
                                       None if ws is None else ws.data_ptr(), n, _stream_handle(stream)))
