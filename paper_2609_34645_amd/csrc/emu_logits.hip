@@ -1112,7 +1112,7 @@ __device__ __forceinline__ void dense_gradient(const Logits& in, const Logits& o
   const uint64_t ri = r * in.row_bytes, ro = r * out.row_bytes;
   const float ref = reference(m, c1);
   const Span span = part_of(block, wave_id(), NW);
-  const int heads = list && span.t0 + lane < span.t1 ? list->head[span.t0 + lane - block.t0] : -1;  // a wave has at most 64 tiles
+  int heads = -1;  // of 64 tiles, one a lane; none of a tile of pads alone
   Reader<TI> from(in, ri, span.t0);
   Cursor<TO, kTile<TI>> to(out, ro, span.t0);
   for (uint32_t tile = span.t0; tile < span.t1; tile += U) {
@@ -1121,6 +1121,10 @@ __device__ __forceinline__ void dense_gradient(const Logits& in, const Logits& o
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (tile + u >= span.t1) break;
+      if (list && (tile + u - span.t0) % 64 == 0) {
+        const uint32_t mine = tile + u + lane;
+        heads = mine < umin(span.t1, tiles<TI>(in.V)) ? list->head[mine - block.t0] : -1;
+      }
       float f[E];
       if constexpr (KIND != ZERO) unpack(x[u], f);
 #pragma unroll
@@ -1134,7 +1138,7 @@ __device__ __forceinline__ void dense_gradient(const Logits& in, const Logits& o
         for (uint32_t e = 0; e < E; ++e)
           if (v + e >= in.V) f[e] = 0.0f;
       }
-      if (list) take_listed(*list, __builtin_amdgcn_readlane(heads, tile + u - span.t0), v, f);
+      if (list) take_listed(*list, __builtin_amdgcn_readlane(heads, (tile + u - span.t0) % 64), v, f);
       store_tile<TO, POL_NT>(out, to, lane, f);
       to.advance(out, 1);
     }
@@ -1168,7 +1172,7 @@ __device__ __forceinline__ void write_row(float* loss, float4* stats, uint64_t r
 constexpr Stats kSkipped = {__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
 
 constexpr int kGradU = 4;
-constexpr int kRowTiles = 1024;  // of a row that one workgroup takes: kMarked columns of fp32
+constexpr int kRowTiles = 1024;  // below V, of a row that one workgroup takes: kMarked columns of fp32
 
 // What the kernels need of the teachers, a wave per row: per entry its column (-1: none, or one that an earlier
 // entry has) and that column's whole probability, per row the mass outside the list (-1: nothing listed). The

@@ -716,6 +716,12 @@ class LogitShards:
         cols = shard_columns(layout)
         return cls(layout, [torch.empty(rows, cols, dtype=dtype, device=device or "cuda") for _ in range(layout.tp)])
 
+    def _here(self, other=None):
+        """The calls launch on the current device: the sets must still be there."""
+        device = _device()
+        if self.device != device or (other is not None and other.device != device):
+            raise ValueError(f"logits on device {self.device}, the current device is {device}")
+
     def workspace(self, k: int = 0, stream=None):
         """(tensor or None, bytes) of a workspace for ``top_logprobs`` (k >= 1) or the distillation calls (k = 0)."""
         key = (self.rows, self.dtype, k)
@@ -788,6 +794,7 @@ def constrain_logits(logits: LogitShards, out: LogitShards = None, tokens=None, 
     int32 [n, words], one per row or chosen by mask_row int32 [rows] (negative: none)."""
     rows, dev, i32, f32 = logits.rows, logits.device, _int32, _float32
     out = logits if out is None else out
+    logits._here(out)
     per_row = (rows,)
     tok = tok_stride = tok_cols = length = prompt = 0
     if tokens is not None:
@@ -827,7 +834,9 @@ def constrain_logits(logits: LogitShards, out: LogitShards = None, tokens=None, 
 
 def top_logprobs(logits: LogitShards, k: int, temperature: float = 1.0, stream=None):
     """``emu_logits_topk``: (index int32 [rows, k], logprob fp32 [rows, k], lse fp32 [rows]) of the k largest logits
-    of every row, in descending order."""
+    of every row, in descending order. What these calls allocate (results, workspaces) belongs to the stream they run on:
+    with ``stream``, wait for it before using results elsewhere."""
+    logits._here()
     ws, n = logits.workspace(k, stream)
     like = logits.tensors[0]
     index = _empty((logits.rows, k), _int32, like, stream)
@@ -851,6 +860,7 @@ def distill_loss(logits: LogitShards, index, teacher, weight=None, temperature: 
     teacher fp32 [rows, k], as ``top_logprobs`` gives them) to the student's softmax at ``temperature``. Returns
     (loss fp32 [rows], stats fp32 [rows, 4]); with ``grad`` also writes the gradient of the losses' sum with respect to
     the logits into its shards (which may be the logits themselves)."""
+    logits._here(grad)
     c = _teacher(logits, index, teacher, weight, "weight", temperature, tail)
     ws, n = logits.workspace(0, stream)
     loss = _empty((logits.rows,), _float32, logits.tensors[0], stream)
@@ -865,6 +875,7 @@ def distill_backward(logits: LogitShards, index, teacher, stats, grad_loss, grad
                      temperature: float = 1.0, tail: bool = False, stream=None) -> LogitShards:
     """``emu_distill_backward``: the gradient with respect to the logits, from the statistics of ``distill_loss`` and the
     gradient grad_loss fp32 [rows] of every row's unweighted loss, into ``grad`` (which may be the logits)."""
+    logits._here(grad)
     c = _teacher(logits, index, teacher, grad_loss, "grad_loss", temperature, tail)
     stats_ptr = _operand(stats, "stats", _float32, (logits.rows, 4), logits.device)
     ws, n = logits.workspace(0, stream)

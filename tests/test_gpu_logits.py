@@ -472,6 +472,120 @@ def test_distill_rows(gpu_lib, rows, tail):
     check_distill(z, index, value, None, 1.0, tail, loss, stats, grad, "bf16")
 
 
+# (vocabulary, tp, pad, dtype): what 4 waves hold at a tile or at 16 each, 8 waves, 16 waves; borders inside tiles, pads
+HELD = [(1024, 2, 0, "bf16"), (4096, 2, 64, "bf16"), (4001, 2, 64, "fp32"), (16000, 3, 8, "bf16"), (40000, 8, 8, "fp32"),
+        (50304, 4, 8, "bf16"), (128256, 8, 128, "bf16")]
+
+
+@pytest.mark.parametrize("V,tp,pad,dtype", HELD)
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_rows_held_in_registers(gpu_lib, V, tp, pad, dtype, tail):
+    """Many aligned rows, which stay in registers between loss and gradient: bit for bit what the same rows give off
+    the vectors' alignment, where they are read again; the small ones against the definition, too."""
+    import torch
+
+    rows, k, tau = 601, 24, 1.3
+    rng = np.random.default_rng(V)
+    lay = layout(V, tp, pad)
+    z = torch.randn(rows, V, device="cuda") * 3
+    z[3], z[5], z[9, ::2] = -float("inf"), 2e7, -3.38e38
+    z[8] = z[8] * 1e6
+    z[11, 7] = float("nan")
+    z[-1, : V // 2] = -float("inf")
+    z = z.to(torch_type(dtype)).double().cpu().numpy()
+    index, value = teacher(V, rows, V, k)
+    index[20], value[21], value[3] = -1, -np.inf, value[3]
+    w = np.float32(rng.uniform(-1, 1, rows))
+    w[rng.random(rows) < 0.3] = 0
+    w[[3, 5, 8, 9, 11, 20, 21]] = 0.5
+    ti, tv, tw = dev(index, np.int32), dev(value, np.float32), dev(w, np.float32)
+    wide = -emu.shard_columns(lay) % 8
+    got = []
+    for skip in (0, 1):
+        student = place(z, lay, dtype, wide=wide, skip=skip)
+        grad = place(np.zeros_like(z), lay, dtype, wide=wide, skip=skip, fill=7.0)
+        loss, stats = emu.distill_loss(student, ti, tv, weight=tw, temperature=tau, tail=tail, grad=grad)
+        got.append([loss, stats] + [t.clone() for t in grad.tensors])
+        if skip == 0:
+            held = grad
+        emu.distill_loss(student, ti, tv, weight=tw, temperature=tau, tail=tail, grad=student)
+        assert same_bits(student.tensors, grad.tensors), "in place"
+    assert same_bits(*got)
+    if V < 5000:
+        check_distill(z, index, value, w, tau, tail, got[0][0], got[0][1], held, dtype)
+
+
+@pytest.mark.parametrize("V,tp,pad", [(266240, 2, 0), (300007, 4, 64), (262100, 2, 65536)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [2, 270])
+def test_wide_vocabularies(gpu_lib, V, tp, pad, dtype, rows):
+    """Rows that no single workgroup takes, and rows whose pads reach beyond what one does."""
+    rng = np.random.default_rng(V)
+    x = rounded(np.tile(rng.normal(0, 3, (2, V)), (rows // 2, 1)), dtype)
+    lay = layout(V, tp, pad)
+    student, grad = place(x, lay, dtype), place(np.zeros_like(x), lay, dtype)
+    top = emu.top_logprobs(student, 64)
+    check_topk(x[:2], [t[:2] for t in top], 64, 1.0)
+    index, value = teacher(V, 2, V, 256, mess=False)
+    index, value = np.tile(index, (rows // 2, 1)), np.tile(value, (rows // 2, 1))
+    loss, stats = emu.distill_loss(student, dev(index, np.int32), dev(value, np.float32), tail=True, grad=grad)
+    part = emu.LogitShards(lay, [t[:2] for t in grad.tensors])
+    check_distill(x[:2], index[:2], value[:2], None, 1.0, True, loss[:2], stats[:2], part, dtype)
+    for t in (*top, loss, stats, *grad.tensors):  # the same two rows again and again
+        assert same_bits([t[-2:]], [t[:2]])
+    c = constraints(1, 2, V, 20)
+    got = place(x[:2], lay, dtype)
+    want, tol = constrained(x[:2], c)
+    apply(got, None, c)
+    close(whole(got)[0], want, tol + np.where(np.isfinite(want), HALF_STEP[dtype] * (np.abs(want) + tol), 0))
+
+
+def test_more_rows_than_a_launch_takes(gpu_lib):
+    import torch
+
+    V, rows, lay = 70, 70001, layout(70, 2, 0)
+    x = rounded(np.random.default_rng(0).normal(0, 3, (1000, V)), "fp32")
+    X = torch.from_numpy(x).float().cuda().repeat(71, 1)[:rows]
+    student = emu.LogitShards(lay, [X[:, :35], X[:, 35:]])
+    index, logp, lse = emu.top_logprobs(student, 9)
+    check_topk(x, (index[:1000], logp[:1000], lse[:1000]), 9, 1.0)
+    grad = emu.LogitShards.alloc(lay, rows, torch.float32)
+    loss, stats = emu.distill_loss(student, index, logp, tail=True, grad=grad)
+    out = emu.LogitShards.alloc(lay, rows, torch.float32)
+    emu.constrain_logits(student, out, tokens=index, seq_len=dev(np.full(rows, 9), np.int32), presence=lse)
+    head = [t[:1000] for t in (index, logp, lse, loss, stats, *grad.tensors, *out.tensors)]
+    for at in (32000, 65000, 69000):
+        assert same_bits(head, [t[at:at + 1000] for t in (index, logp, lse, loss, stats, *grad.tensors, *out.tensors)])
+    d = ol.distill(x, index[:1000].cpu().numpy(), logp[:1000].cpu().numpy(), None, 1.0, True)
+    assert np.abs(loss[:1000].double().cpu().numpy() - d["loss"]).max() < 1e-5  # 0 but for rounding: student and teacher agree
+
+
+@pytest.mark.parametrize("rows", [3, 600])
+def test_topk_many_ties(gpu_lib, rows):
+    """More logits at the bound than the list holds, in rows shared by workgroups and in rows of their own."""
+    V, lay = 20003, layout(20003, 2, 1)
+    rng = np.random.default_rng(rows)
+    x = np.tile(np.stack([rng.integers(0, 2, V), np.full(V, -1.5), np.arange(V) // 64 * 0.5]).astype(float), (rows // 3, 1))
+    got = emu.top_logprobs(place(x, lay, "fp32"), 64)
+    check_topk(x[:3], [t[:3] for t in got], 64, 1.0)
+    assert same_bits([t[-3:] for t in got], [t[:3] for t in got])
+
+
+@pytest.mark.parametrize("tau", [1e-6, 1e-3, 1e6])
+@pytest.mark.parametrize("tail", [False, True])
+def test_far_temperatures(gpu_lib, tau, tail):
+    V, rows, k = 1500, 4, 10
+    z = rounded(np.random.default_rng(5).normal(0, 3, (rows, V)), "fp32")
+    index, value = teacher(6, rows, V, k, mess=False)
+    lay = layout(V, 2, 0)
+    check_topk(z, emu.top_logprobs(place(z, lay, "fp32"), k, tau), k, tau)
+    if tail and tau < 1:  # a q of e^-1000 and less is 0 in the row's sum, and the loss infinite by definition of the tail's log
+        return
+    grad = place(np.zeros_like(z), lay, "fp32")
+    loss, stats = emu.distill_loss(place(z, lay, "fp32"), dev(index, np.int32), dev(value, np.float32), temperature=tau, tail=tail, grad=grad)
+    check_distill(z, index, value, None, tau, tail, loss, stats, grad, "fp32")
+
+
 # ----------------------------------------------------------------------------------------------------
 # together, and how they are called
 # ----------------------------------------------------------------------------------------------------
