@@ -378,7 +378,7 @@ int emu_check_bucket_tables(emu_plan_t plan, int32_t side, uint64_t bucket_bytes
  *
  *   - Logits of layout *layout (vocabulary V, padded to Vp columns): tp shards, shard t holding columns
  *     [t*Vp/tp, (t+1)*Vp/tp) of every row. The layout's dtype is its weights'; the logits have their own.
- *     Columns from V on (pad rows of the LM head) are never read; output shards get the value stated there.
+ *     What columns from V on hold (pad rows of the LM head) does not count; output shards get the value stated there.
  *   - Shard addresses come in a HOST array, which the call copies (logits are new each step; a device table
  *     would need an upload each time). A shard starts at any multiple of its element size; rows are
  *     row_stride elements apart, the same in all shards of one set. Columns past Vp/tp are not touched.

@@ -1,7 +1,7 @@
 // Operators on the logits of a vocab-parallel LM head (include/emu.h): constraints ahead of sampling, the
 // k largest log-probabilities, distillation with its gradient. Every row is read once (twice for a loss with its
-// gradient), in 16-byte vectors; every reduction runs over global columns in a fixed order, so that no result
-// depends on how the shards cut them.
+// gradient where registers do not hold it), in 16-byte vectors; every reduction runs over global columns in a fixed
+// order, so that no result depends on how the shards cut them.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -42,8 +42,8 @@ template <typename T> __device__ __forceinline__ T scalar(const T* p) { return *
 // ------------------------------------------------------------------------------------------------
 // A lane holds 16 bytes, kE<T> columns from a multiple of kE<T> on; a wave's tile is 64 such vectors, 1 KB. A workgroup
 // has a span of tiles and each of its waves a contiguous part of it, U tiles at a time: copies of rows ran at 6.3 TB/s
-// with 16 contiguous KB per wave, at 5.5 with the waves' 4 KB by turns. Columns are counted over the whole vocabulary, so
-// which lane adds up which column, and in which order, does not depend on the shards. Where the U tiles lie inside
+// with 16 contiguous KB per wave, at 5.5 with the waves' 4 KB by turns. Columns are counted over the whole vocabulary,
+// so which lane adds up which column, and in which order, does not depend on the shards. Where the U tiles lie inside
 // one shard (all but one stretch per shard do), they are U loads from one scalar base at any element alignment;
 // elsewhere every lane finds its own shard, and a vector across a shard's end is put together by element.
 
@@ -364,8 +364,7 @@ __device__ __forceinline__ float true_sum(Running r, float c1) {
   return r.s * __builtin_amdgcn_exp2f(-fmaf(r.m, c1, -reference(r.m, c1)));
 }
 
-// Sum of exp((x - m) / tau) over the row by the whole workgroup; marked columns (a bit each from column 0 on) are
-// left out.
+// Sum of exp((x - m) / tau) over the row by the whole workgroup, without the k listed columns.
 template <typename T, int NW>
 __device__ float careful_sum(const Logits& l, uint64_t row_off, float m, float c1, const int32_t* listed, int k, float* lds) {
   float s = 0.0f;
@@ -395,13 +394,16 @@ __device__ __forceinline__ float log_prob(float x, float m, float s, float c1) {
 // forbids whole, and in place, where most vectors stay as they are); meanwhile it goes over the row's history and
 // counts the slice's tokens in LDS (integer atomics: any order gives the same counts). The slice's biases lie in
 // LDS in list order, the first of a column with the sum of all of them. Then every vector is copied, masked or
-// changed once: a column's word says all that concerns it, 0 that nothing does.
+// changed once: a column's word says all that concerns it, 0 that nothing does. 256 fp32 rows of 128,256,
+// all under a mask, take 53 us with one token of history (195 MB, 3.7 TB/s) and 73 with up to 32,768 (20,480 on
+// average): every slice goes over the whole history. 64 bf16 rows take 14.6 us, one round of workgroups whose loads
+// follow from one another.
 
 constexpr uint32_t kSeen = 1u << 31, kCountBits = (1u << 20) - 1;
 constexpr uint32_t kSlotShift = 20, kSlotBits = 1023;  // of the column's first bias, from 1 on; kSlotBits: not in the list
 constexpr int kListed = 512;                           // biases of a slice held in LDS
-// Workgroups of 512 threads on 8,192 columns took 14.8 us for 64 rows of 128,256 with histories of 2,500 (256 threads 15.4);
-// 1,024 threads on 16,384 took 73 us for 256 rows with 20,480 (on 32,768 77, 512 threads 84).
+// Workgroups of 512 threads on 8,192 columns took 14.8 us for 64 rows of 128,256 with histories of 2,500 (256 threads
+// 15.4); 1,024 threads on 16,384 took 73 us for 256 rows with 20,480 (on 32,768 77, 512 threads 84).
 constexpr int32_t kLongHistory = 8192;
 
 template <typename TI, typename TO, int NT, uint32_t SLICE>
@@ -611,7 +613,9 @@ __global__ __launch_bounds__(NT) void k_constrain(Logits in, Logits out, emu_con
 // largest of the threads' maxima is a bound that k logits reach; about k + k^2 / (2 threads) do in all, in as many
 // stretches. Those stretches are read again by their lanes, and what reaches the bound is sorted. Where that is more
 // than the LDS list holds (ties at the bound, a few threads with all large logits), each wave goes over its tiles again
-// with its own k best sorted, one per lane, and merges in what beats its k-th, 64 at a time.
+// with its own k best sorted, one per lane, and merges in what beats its k-th, 64 at a time. 4,096 rows of 128,256 in
+// bf16, k 64: 195 to 207 us (5.1 to 5.4 TB/s); an earlier form, whose waves kept sorted lists during the scan, took
+// 402.
 
 __device__ __forceinline__ uint32_t top_order(float x) {  // 0: never chosen
   const uint32_t u = __float_as_uint(x + 0.0f);  // -0 becomes 0
@@ -877,8 +881,10 @@ __global__ __launch_bounds__(kTopParts * 64) void k_topk_join(Logits in, uint32_
 // the workspace, a second kernel joins them to the row's, and the gradient goes by parts again (in place, no part
 // may be written before every reader of the row is done: hence the kernel between).
 // The gradient is coef * exp((z - m) / tau), but for the listed columns, whose gradients come from their entries'
-// threads by way of LDS. With a tail the scan leaves out the listed
-// columns (a bit each in LDS), so that a small mass outside the list is a sum of its own and no difference.
+// threads by way of LDS. 4,096 rows of 128,256 in bf16, all with a weight: the loss 195 to 204 us
+// (5.2 to 5.4 TB/s), the loss with the gradient 426 to 430 (4.9 TB/s), the gradient alone 390 over four shards and 364
+// in one (5.4 and 5.8 TB/s). With a tail the scan leaves out the listed columns (a bit each in LDS), so that a small
+// mass outside the list is a sum of its own and no difference.
 
 // A list of log-probabilities rounded to fp32 can miss a sum of 1 by sum p |log p| 2^-24 < 2^-20.
 constexpr float kRestNoise = 0x1p-20f;
@@ -1281,11 +1287,12 @@ __global__ __launch_bounds__(NW * 64) void k_distill(Logits in, Logits grad, emu
 // A row held in registers between its two uses, up to NV tiles of each of NW waves, where the shards hold whole aligned
 // vectors and are no shorter than a tile (a tile then lies in one shard or two): one read, one write. The
 // workgroups stay and take rows by ticket, so that the device works on a window of neighbouring rows (in equal shares
-// fixed ahead, 4,096 rows of 131,072 took 450 us against 425) and rows without a weight cost no one more; while a vector's gradient leaves, the next row's vector is loaded into its
-// registers, so that memory has both to do. Every turn issues the same loads and stores, whatever the row: a wait
-// for one of them can then name the number of younger ones, where with any in doubt it would be for all. Tiles that
-// a wave does not have, and rows without a weight, load a vector of -infinities; a store beyond a shard's row is
-// dropped by the buffer's bounds. Tiles, and the order of every sum, are k_distill's: the result is the same, bit for bit.
+// fixed ahead, 4,096 rows of 131,072 took 450 us against 425) and rows without a weight cost no one more; while a
+// vector's gradient leaves, the next row's vector is loaded into its registers, so that memory has both to do. Every
+// turn issues the same loads and stores, whatever the row: a wait for one of them can then name the number of younger
+// ones, where with any in doubt it would be for all. Tiles that a wave does not have, and rows without a weight, load a
+// vector of -infinities; a store beyond a shard's row is dropped by the buffer's bounds. Tiles, and the order of every
+// sum, are k_distill's: the result is the same, bit for bit.
 constexpr int kResidentTiles = 16;
 __device__ const v4u kNoLogits[2] = {{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}, {0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}};
 
@@ -1681,6 +1688,9 @@ struct DistillWorkspace {
 
 // Whether k_distill_resident takes these rows.
 constexpr int64_t kResidentRows = 256;
+// The loss alone: below, the row's own workgroup takes its teacher, a launch less (40 us against 42 for 509 rows of
+// 128,256; 85 against 77 for 1,500).
+constexpr int64_t kPreparedLossRows = 1024;
 #ifndef LOSST
 #define LOSST 256
 #endif
@@ -1845,7 +1855,7 @@ int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float
           if (grad) launch_backward(ti, grad->dtype, n, st, li, lo, *teacher, c1, stats, ws, r0);
           return;
         }
-        const bool prepared = student->rows >= kResidentRows;
+        const bool prepared = student->rows >= (grad ? kResidentRows : kPreparedLossRows);
         if (prepared) launch_prepare(n, st, *teacher, li.V, ws, r0);
         by_waves(n_tiles, [&](auto waves) {
           constexpr int NW = decltype(waves)::value;
