@@ -403,7 +403,7 @@ constexpr uint32_t kSeen = 1u << 31, kCountBits = (1u << 20) - 1;
 constexpr uint32_t kSlotShift = 20, kSlotBits = 1023;  // of the column's first bias, from 1 on; kSlotBits: not in the list
 constexpr int kListed = 512;                           // biases of a slice held in LDS
 // Workgroups of 512 threads on 8,192 columns took 14.8 us for 64 rows of 128,256 with histories of 2,500 (256 threads
-// 15.4); 1,024 threads on 16,384 took 73 us for 256 rows with 20,480 (on 32,768 77, 512 threads 84).
+// 15.4); 1,024 threads on 16,384 took 73 us for 256 rows with 20,480 on average (on 32,768 77, 512 threads 84).
 constexpr int32_t kLongHistory = 8192;
 
 template <typename TI, typename TO, int NT, uint32_t SLICE>
@@ -630,7 +630,6 @@ __device__ __forceinline__ float order_value(uint32_t order) {
 }
 __device__ __forceinline__ float key_value(uint64_t key) { return order_value(uint32_t(key >> 32)); }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
 __device__ __forceinline__ uint64_t lane_key(uint64_t x, uint32_t lane) {  // the same lane everywhere
   return uint64_t(__builtin_amdgcn_readlane(uint32_t(x >> 32), lane)) << 32 | uint32_t(__builtin_amdgcn_readlane(uint32_t(x), lane));
 }
@@ -1691,10 +1690,6 @@ constexpr int64_t kResidentRows = 256;
 // The loss alone: below, the row's own workgroup takes its teacher, a launch less (40 us against 42 for 509 rows of
 // 128,256; 85 against 77 for 1,500).
 constexpr int64_t kPreparedLossRows = 1024;
-#ifndef LOSST
-#define LOSST 256
-#endif
-constexpr uint32_t kLossTiles = LOSST;
 template <typename TI>
 static bool holds(const Logits& in, const Logits& out, uint64_t out_size) {
   uint64_t bits = in.row_bytes | out.row_bytes;
