@@ -1408,11 +1408,9 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill_resident(Logits in, Logi
     const float ref = reference(st.m, c1);
     if (!zero) coef = scale * st.factor * ((wild ? 1.0f : __builtin_amdgcn_exp2f(-fmaf(st.m, c1, -ref))) / st.s);
     int heads = -1;
-    if (!dead) {
-      chain<TI>(list, 0, e, entry_gradient(e, st, c1, scale));
-      __syncthreads();
-      if (t0 + lane < t1) heads = list.head[t0 + lane];
-    }
+    if (!dead) chain<TI>(list, 0, e, entry_gradient(e, st, c1, scale));
+    if (live) __syncthreads();  // the chains are whole, and no wave reads t.sum for conclude any more
+    if (!dead && t0 + lane < t1) heads = list.head[t0 + lane];
     if (wild) dense_gradient<TI, TO, 1, NW, POL_NT, ANY_RANGE>(in, grad, r, {0, tiles<TI>(in.V)}, &list, st.m, c1, coef);
     const bool write = now < rows && !wild;
     Reader<TI> from(in, rn, t0);
