@@ -294,7 +294,8 @@ __device__ __forceinline__ T block_reduce(T x, T* lds, F f) {
 
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 __device__ __forceinline__ double addd(double a, double b) { return a + b; }
-__device__ __forceinline__ float max3(float a, float b, float c) {  // a NaN is passed over
+// A quiet NaN is passed over; a signalling one is too, but what came before it may go with it.
+__device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
@@ -339,7 +340,8 @@ __device__ __forceinline__ Running block_joined(Running a, Running* lds, float c
   return waves_joined<NW>(lds, c1);
 }
 
-// U vectors of a lane; gives their largest value.
+// U vectors of a lane; gives their largest value. Where they hold a NaN the sum is NaN from here on, and both the result
+// and r.m are some of the lane's values, if perhaps not the largest.
 template <int U, uint32_t E>
 __device__ __forceinline__ float add_values(Running& r, const float (&f)[U][E], float c1) {
   float top = f[0][0];
@@ -788,7 +790,7 @@ __global__ __launch_bounds__(NW * 64) void k_topk(Logits in, uint32_t k, float c
       for (int u = 0; u < U; ++u) unpack(x[u], f[u]);
       top = fmaxf(top, add_values<U, E>(run, f, c1));
       if (tile + U >= segment_end || tile + U >= span.t1) {
-        t.segment[segment][threadIdx.x] = top;
+        t.segment[segment][threadIdx.x] = run.s == run.s ? top : __builtin_nanf("");  // behind a NaN: any value
         ++segment;
         segment_end += per;
         top = -kInf;
@@ -803,7 +805,7 @@ __global__ __launch_bounds__(NW * 64) void k_topk(Logits in, uint32_t k, float c
   const uint32_t kth = t.order[k - 1];
   const float level = order_value(kth);
   __syncthreads();
-  // the stretches that hold what reaches it, and from them, a vector a thread, what does
+  // the stretches that hold (or, NaN, may hold) what reaches it, and from them, a vector a thread, what does
   const uint32_t stretches = per ? (span.t1 - span.t0 + per - 1) / per : 0;
   for (uint32_t i = 0; i < stretches; ++i)
     if (!(t.segment[i][threadIdx.x] < level)) {
