@@ -30,7 +30,7 @@ TINY = (2, 256, 4, 64, 2, 688, 1024)
 ONE_B = (16, 2048, 32, 64, 8, 8192, 128256)
 PMC_SUMMARY = os.path.join(ROOT, "profiles", "reshard_8b_tp2pp2_tp4pp1_pmc.txt")
 KERNEL_SRCS = [os.path.join(ROOT, "paper_2609_34645_amd", "csrc", f)
-               for f in ("emu_exec.hip", "emu_internal.h", "emu_plan.cpp", "emu_launch.cpp")]
+               for f in ("emu_exec.hip", "emu_hip.h", "emu_internal.h", "emu_plan.cpp", "emu_launch.cpp")]
 
 
 def log(*a):
