@@ -248,8 +248,16 @@ class Model:
         return cls(*t)
 
 
+class _KeepsHead:
+    """Room for what ``_head`` keeps with a layout, beside its fields: they alone are in ``vars``, copies and pickles."""
+    __slots__ = ("_head",)
+
+    def __getstate__(self):
+        return self.__dict__.copy()
+
+
 @dataclass(frozen=True)
-class Layout:
+class Layout(_KeepsHead):
     model: Model
     tp: int
     pp: int
@@ -664,13 +672,15 @@ def shard_columns(layout: Layout) -> int:
 
 def _head(layout):
     """(C layout, columns per shard, workspace sizes), kept with the layout, which never changes."""
-    head = layout.__dict__.get("_head")
-    if head is None:
-        c = layout.c()
-        check(load().emu_layout_check(ctypes.byref(c)))
-        q = layout.tp * layout.pad
-        head = (ctypes.pointer(c), (-(-layout.model.vocab // q) * q if q else layout.model.vocab) // layout.tp, {})
-        object.__setattr__(layout, "_head", head)
+    try:
+        return layout._head
+    except AttributeError:
+        pass
+    c = layout.c()
+    check(load().emu_layout_check(ctypes.byref(c)))
+    q = layout.tp * layout.pad
+    head = (ctypes.pointer(c), (-(-layout.model.vocab // q) * q if q else layout.model.vocab) // layout.tp, {})
+    object.__setattr__(layout, "_head", head)
     return head
 
 
@@ -680,7 +690,7 @@ class LogitShards:
     shards have one dtype and one row stride."""
 
     def __init__(self, layout: Layout, tensors):
-        c, cols, self._sizes = layout.__dict__.get("_head") or _head(layout)
+        c, cols, self._sizes = _head(layout)
         tensors = list(tensors)
         if len(tensors) != layout.tp:
             raise ValueError(f"{len(tensors)} shards, the layout has tp={layout.tp}")
