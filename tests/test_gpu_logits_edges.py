@@ -1,9 +1,10 @@
-"""The operators on an LM head's logits where inputs and calls are unusual: signalling NaNs."""
+"""The operators on an LM head's logits where inputs and calls are unusual: signalling NaNs, inputs that another stream
+is still writing."""
 import numpy as np
 import pytest
 
 from paper_2609_34645_amd import emu
-from tests.test_gpu_logits import check_topk, dev, layout, place, rounded, teacher
+from tests.test_gpu_logits import check_topk, constraints, dev, layout, packed, place, rounded, same_bits, teacher
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +77,58 @@ def test_signalling_nans_reach_the_loss(gpu_lib, V, tp, rows, tail):
     assert torch.equal(loss[~bad], wl[~bad]) and torch.equal(stats[~bad], ws[~bad])
     for a, b, c in zip(g.tensors, want.tensors, back.tensors):
         assert a[bad].isnan().all() and c[bad].isnan().all() and torch.equal(a[~bad], b[~bad])
+
+
+@pytest.mark.parametrize("explicit", [False, True])
+@pytest.mark.parametrize("V,tp,rows", [(50257, 1, 6), (50304, 4, 300)])
+def test_calls_wait_for_their_own_stream_alone(gpu_lib, V, tp, rows, explicit):
+    """Every operator reads what its stream writes late: the real logits are copied over others behind long work, and no
+    host call waits between. `explicit`: by stream=, from another current stream."""
+    import contextlib
+
+    import torch
+
+    lay = layout(V, tp, 0)
+    rng = np.random.default_rng(V)
+    index, value = teacher(3, rows, V, 12, mess=False)
+    ti, tv, w = dev(index, np.int32), dev(value, np.float32), dev(rng.uniform(0.5, 1, rows), np.float32)
+    c = constraints(2, rows, V, 60)
+    limits = dict(tokens=dev(c["tokens"], np.int32), seq_len=dev(c["seq_len"], np.int32), presence=dev(c["presence"], np.float32),
+                  mask=dev(packed(c["allowed"]), np.int32), mask_row=dev(c["mask_row"], np.int32))
+    real, late = (emu.LogitShards.alloc(lay, rows, torch.bfloat16) for _ in range(2))
+    outs = [[emu.LogitShards.alloc(lay, rows, torch.bfloat16) for _ in range(3)] for _ in range(2)]
+    for t in real.tensors:
+        t.normal_(0, 3)
+
+    def calls(logits, out, stream):
+        emu.constrain_logits(logits, out[0], stream=stream, **limits)
+        top = emu.top_logprobs(out[0], 9, stream=stream)
+        loss, stats = emu.distill_loss(logits, ti, tv, weight=w, tail=True, grad=out[1], stream=stream)
+        emu.distill_backward(logits, ti, tv, stats, w, out[2], tail=True, stream=stream)
+        return [*top, loss, stats]
+
+    a = torch.cuda.Stream()
+    work = torch.randn(4096, 4096, device="cuda")
+    want = calls(real, outs[0], None)
+    with torch.cuda.stream(a):
+        work = work @ work * 1e-3  # the library's own first-call work is over
+    calls(real, outs[1], a)
+    torch.cuda.synchronize()
+    for turn in range(2):
+        for t in late.tensors + [t for o in outs[1] for t in o.tensors]:
+            t.fill_(turn + 1)
+        torch.cuda.synchronize()
+        done = torch.cuda.Event()
+        with torch.cuda.stream(a):
+            for _ in range(60):
+                work = work @ work * 1e-3
+            for dst, src in zip(late.tensors, real.tensors):
+                dst.copy_(src)
+        with contextlib.nullcontext() if explicit else torch.cuda.stream(a):
+            got = calls(late, outs[1], a if explicit else None)
+        done.record(a)
+        assert not done.query(), "the long work was over before the calls were made"
+        a.synchronize()
+        assert same_bits(got, want)
+        for x, y in zip(outs[1], outs[0]):
+            assert same_bits(x.tensors, y.tensors)
