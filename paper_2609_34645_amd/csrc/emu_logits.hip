@@ -1285,8 +1285,8 @@ __global__ __launch_bounds__(NW * 64) void k_distill(Logits in, Logits grad, emu
   if constexpr (GRAD) row_gradient<TI, TO, kGradU, NW, POL_NT>(in, grad, r, {0, tiles<TI>(in.Vp)}, list, e, st, c1, w, rest < 0.0f);
 }
 
-// A row held in registers between its two uses, up to NV tiles of each of NW waves, where the shards hold whole aligned
-// vectors and are no shorter than a tile (a tile then lies in one shard or two): one read, one write. The
+// A row held in registers between its two uses, up to 16 tiles of each of NW waves, where the shards hold whole aligned
+// vectors and are no shorter than a tile (a tile then lies in one shard or two): one read, one write, no tail. The
 // workgroups stay and take rows by ticket, so that the device works on a window of neighbouring rows (in equal shares
 // fixed ahead, 4,096 rows of 131,072 took 450 us against 425) and rows without a weight cost no one more; while a
 // vector's gradient leaves, the next row's vector is loaded into its registers, so that memory has both to do. Every
@@ -1312,24 +1312,20 @@ __device__ __forceinline__ void store_bounded(__amdgpu_buffer_rsrc_t to, uint32_
   }
 }
 
-template <typename TI, typename TO, int NW, int NV, bool TAIL>
+template <typename TI, typename TO, int NW>
 __global__ __launch_bounds__(NW * 64, 4) void k_distill_resident(Logits in, Logits grad, emu_teacher_t te, float c1, float* loss, float4* stats,
                                                                      const Prepared* teacher, const float* rests, uint32_t* ticket, uint32_t rows,
                                                                      uint64_t row0) {
-  constexpr int U = kScanU;
+  constexpr int U = kScanU, NV = kResidentTiles;
   constexpr uint32_t E = kE<TI>;
-  extern __shared__ uint32_t bits[];
   __shared__ DistillLds<NW> t;
   __shared__ Listed<NW * NV> list;
-  __shared__ Running inside_run[NW];
   __shared__ uint8_t* shards[kMaxShards];
   v4u x[NV];
   __shared__ uint32_t taken, first;
   uint32_t now = rows, next, after;  // the row in x, the row to load, the one behind it; `rows`: none
   float w = 0.0f;
   Entry e = {-1, 0.0f, -kInf};
-  if constexpr (TAIL)
-    for (uint32_t i = threadIdx.x; i < tiles<TI>(in.V) * kTile<TI> / 32; i += NW * 64) bits[i] = 0;
   for (int i = threadIdx.x; i < NW * NV; i += NW * 64) list.head[i] = -1;
   if (threadIdx.x < kMaxShards) shards[threadIdx.x] = in.p[threadIdx.x];
   if (threadIdx.x == 0) first = atomicAdd(ticket, 1u);
@@ -1350,13 +1346,9 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill_resident(Logits in, Logi
     v2u f_next = {~0u, 0u};
     if (w_next != 0.0f && int(thread) < te.k) f_next = ld8_any<POL_PLAIN>(reinterpret_cast<const uint8_t*>(teacher + next), thread * 8);
     Stats st = kSkipped;
-    float rest = 0.0f, rest_loss = 0.0f, scale = 0.0f, coef = 0.0f;
+    float rest_loss = 0.0f, scale = 0.0f, coef = 0.0f;
     const bool live = now < rows && w != 0.0f;
     if (live) {
-      if constexpr (TAIL) {
-        if (e.col >= 0) atomicOr(&bits[e.col / 32], 1u << (e.col % 32));
-        __syncthreads();
-      }
       Running run = {-kInf, 0.0f};
 #pragma unroll
       for (int i = 0; i < NV; i += U) {
@@ -1365,8 +1357,6 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill_resident(Logits in, Logi
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           asm volatile("" : "+v"(x[i + u]));  // in this order: all at once would take twice the registers
-          if constexpr (TAIL)
-            if (t0 + i + u < t1) leave_out<TI>(x[i + u], bits, (t0 + i + u) * kTile<TI> + lane * E);
           if (t0 + i + u == last) {  // pads behind V in V's own vector
 #pragma unroll
             for (uint32_t q = 0; q < E; ++q)
@@ -1379,24 +1369,13 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill_resident(Logits in, Logi
       }
       run = wave_joined(run, c1);
       if (lane == 0) t.run[wave_id()] = run;
-      if constexpr (TAIL) {
-        const Running in_list = wave_joined(entry_run(e, c1), c1);
-        if (lane == 0) inside_run[wave_id()] = in_list;
-      }
-      if (int(threadIdx.x) < kMaxTeacher) t.col[threadIdx.x] = e.col;
     }
-    rest = live ? scalar(rests + now) : 0.0f;
+    const bool listed = live && !(scalar(rests + now) < 0.0f);
     if (threadIdx.x == 0) taken = later;  // everyone has read the last one before the last turn's last barrier
     __syncthreads();
     after = umin(__builtin_amdgcn_readfirstlane(taken), rows);
     if (live) {
-      Running inside = {-kInf, 0.0f};
-      const Running run = waves_joined<NW>(t.run, c1);
-      if constexpr (TAIL) {
-        inside = waves_joined<NW>(inside_run, c1);
-        if (e.col >= 0) bits[e.col / 32] = 0;
-      }
-      st = conclude<TI, NW, TAIL>(in, ri, run, inside, e, rest < 0.0f ? 0.0f : rest, te.k, c1, t, &rest_loss);
+      st = conclude<TI, NW, false>(in, ri, waves_joined<NW>(t.run, c1), {-kInf, 0.0f}, e, 0.0f, 0, c1, t, &rest_loss);
       scale = w * (c1 * 0.69314718f);
     }
     const uint64_t ro = r * grad.row_bytes, rn = (row0 + next) * in.row_bytes;
@@ -1405,14 +1384,13 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill_resident(Logits in, Logi
       const uint32_t t = shard_of(in, f_next[0]);
       z_next = reinterpret_cast<const TI*>(shards[t] + rn)[f_next[0] - t * in.cols];
     }
-    const bool dead = !live || rest < 0.0f;
-    const bool zero = dead || st.s == 0.0f, wild = !zero && !plain(st.m, c1);
+    const bool zero = !listed || st.s == 0.0f, wild = !zero && !plain(st.m, c1);
     const float ref = reference(st.m, c1);
     if (!zero) coef = scale * st.factor * ((wild ? 1.0f : __builtin_amdgcn_exp2f(-fmaf(st.m, c1, -ref))) / st.s);
     int heads = -1;
-    if (!dead) chain<TI>(list, 0, e, entry_gradient(e, st, c1, scale));
+    if (listed) chain<TI>(list, 0, e, entry_gradient(e, st, c1, scale));
     if (live) __syncthreads();  // the chains are whole, and no wave reads t.sum for conclude any more
-    if (!dead && t0 + lane < t1) heads = list.head[t0 + lane];
+    if (listed && t0 + lane < t1) heads = list.head[t0 + lane];
     if (wild) dense_gradient<TI, TO, 1, NW, POL_NT, ANY_RANGE>(in, grad, r, {0, tiles<TI>(in.V)}, &list, st.m, c1, coef);
     const bool write = now < rows && !wild;
     Reader<TI> from(in, rn, t0);
@@ -1458,7 +1436,7 @@ __global__ __launch_bounds__(NW * 64, 4) void k_distill_resident(Logits in, Logi
     if (lane == 0) t.sum[wave_id()] = part;
     __syncthreads();
     if (now < rows) {
-      if (!dead && e.col >= 0) list.head[e.col / kTile<TI>] = -1;
+      if (listed && e.col >= 0) list.head[e.col / kTile<TI>] = -1;
       float total = t.sum[0];
 #pragma unroll
       for (int i = 1; i < kMaxTeacher / 64; ++i) total += t.sum[i];
@@ -1685,11 +1663,29 @@ struct DistillWorkspace {
   }
 };
 
-// Whether k_distill_resident takes these rows.
-constexpr int64_t kResidentRows = 256;
-// The loss alone: below, the row's own workgroup takes its teacher, a launch less (40 us against 42 for 509 rows of
-// 128,256; 85 against 77 for 1,500).
-constexpr int64_t kPreparedLossRows = 1024;
+// Below, the row's own workgroup takes its teacher, a launch less. The loss alone: 33 us against 34 (prepared) for 511
+// bf16 rows of 128,256, 57 against 53 for 1,000; narrow rows gain less from the preparation: 36 against 39 for 2,048 of 32,768.
+// With the gradient: 38 against 40 for 255 of 128,256, 62 against 58 for 384; 24 against 27 for 511 of 32,768.
+constexpr int64_t kPreparedLossRows = 1024, kPreparedGradRows = 256;
+
+// Whether k_distill_resident takes these rows. Reading them again instead costs less than it looks: the second read of the rows in work comes
+// from the last-level cache, and nothing waits for a row's turn. Registers pay where
+//  * there is no tail (its marks and second statistics spilled: 4,096 bf16 rows of 128,256 took 529 us held, 495 read again) and
+//    the gradient is no wider than the logits (bf16 to fp32, 2 GiB: 558 to 561 us held, 507 to 556 read again);
+//  * a wave holds enough of them: rows of 4,032 bf16 columns (8 tiles) took 989 us held, 555 read again, 1 GiB in all; 40,896
+//    (80 tiles, 8 waves of 10) 497 and 477 at 2 GiB, 51,136 (13 a wave) 477 and 485; fp32 from 64 tiles on (20,416, 80 tiles:
+//    235 and 251 at 1 GiB, 12,224, 48 tiles: 254 and 267, but 158 and 153 at half of it);
+//  * the call moves enough bytes that most of them miss the cache: bf16 rows of 128,448 took 156 us held and 153 read
+//    again at 0.5 GiB read and written, 251 and 271 at 1 GiB, 460 and 504 at 2; fp32 rows of 64,192 87 and 86 at 0.25, 133
+//    and 138 at 0.5, 226 and 253 at 1.
+template <typename TI, typename TO, bool TAIL>
+constexpr bool kMayStay = !TAIL && sizeof(TO) <= sizeof(TI);
+template <typename TI, typename TO>
+static bool worth_holding(const Logits& in, uint32_t rows) {
+  const uint32_t n = tiles<TI>(in.V);
+  const uint64_t bytes = uint64_t(rows) * in.V * (sizeof(TI) + sizeof(TO));
+  return n >= 4u * kResidentTiles && (sizeof(TI) == 4 ? bytes >= 1u << 29 : n > 10u * uint32_t(row_waves(n)) && bytes >= 1u << 30);
+}
 template <typename TI>
 static bool holds(const Logits& in, const Logits& out, uint64_t out_size) {
   uint64_t bits = in.row_bytes | out.row_bytes;
@@ -1850,7 +1846,7 @@ int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float
           if (grad) launch_backward(ti, grad->dtype, n, st, li, lo, *teacher, c1, stats, ws, r0);
           return;
         }
-        const bool prepared = student->rows >= (grad ? kResidentRows : kPreparedLossRows);
+        const bool prepared = student->rows >= (grad ? kPreparedGradRows : kPreparedLossRows);
         if (prepared) launch_prepare(n, st, *teacher, li.V, ws, r0);
         by_waves(n_tiles, [&](auto waves) {
           constexpr int NW = decltype(waves)::value;
@@ -1861,13 +1857,14 @@ int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float
           if (!grad) return launch(k_distill<TI, TI, NW, TAIL, false>);
           by_type(grad->dtype, [&](auto to) {
             using TO = decltype(to);
-            if (!prepared || !holds<TI>(li, lo, sizeof(TO))) return launch(k_distill<TI, TO, NW, TAIL, true>);
-            auto stay = [&](auto kernel) {
-              hipLaunchKernelGGL(kernel, dim3(std::min(n, cus * (16 / NW))), dim3(NW * 64), marks, st, li, lo, *teacher, c1, d_loss, stats,
-                                 ws.teacher, ws.rests, ws.ticket, n, r0);
-            };
-            if (NW == 4 && n_tiles <= 16) stay(k_distill_resident<TI, TO, 4, 4, TAIL>);
-            else stay(k_distill_resident<TI, TO, NW, kResidentTiles, TAIL>);
+            if constexpr (kMayStay<TI, TO, TAIL>) {
+              if (prepared && worth_holding<TI, TO>(li, n) && holds<TI>(li, lo, sizeof(TO))) {
+                hipLaunchKernelGGL((k_distill_resident<TI, TO, NW>), dim3(std::min(n, cus * (16 / NW))), dim3(NW * 64), 0, st, li, lo, *teacher, c1,
+                                   d_loss, stats, ws.teacher, ws.rests, ws.ticket, n, r0);
+                return;
+              }
+            }
+            launch(k_distill<TI, TO, NW, TAIL, true>);
           });
         });
       };
