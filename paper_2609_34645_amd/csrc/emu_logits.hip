@@ -404,8 +404,10 @@ __device__ __forceinline__ float log_prob(float x, float m, float s, float c1) {
 constexpr uint32_t kSeen = 1u << 31, kCountBits = (1u << 20) - 1;
 constexpr uint32_t kSlotShift = 20, kSlotBits = 1023;  // of the column's first bias, from 1 on; kSlotBits: not in the list
 constexpr int kListed = 512;                           // biases of a slice held in LDS
-// Workgroups of 512 threads on 8,192 columns took 14.8 us for 64 rows of 128,256 with histories of 2,500 (256 threads
-// 15.4); 1,024 threads on 16,384 took 73 us for 256 rows with 20,480 on average (on 32,768 77, 512 threads 84).
+// Of a history's capacity: up to it 512 threads take 8,192 columns, beyond it 1,024 threads 16,384, so that half as many
+// workgroups go over a history. 256 rows of 128,256, histories of 62% of the capacity on average, us: 8,192 tokens bf16 42 / 44, fp32
+// 60 / 61; 16,384 48 / 48 and 66 / 66; 32,768 58 / 55 and 77 / 72 (256 rows of 32,768 27 / 20). The host knows the capacity
+// alone: a buffer of the model's longest sequence that holds short ones pays up to 3 us of 34 for the long form.
 constexpr int32_t kLongHistory = 8192;
 
 template <typename TI, typename TO, int NT, uint32_t SLICE>
@@ -1514,12 +1516,18 @@ __global__ __launch_bounds__(NW * 64) void k_distill_backward(Logits in, Logits 
   row_gradient<TI, TO, kGradU, NW, POL_NT>(in, grad, r, block, list, e, st, c1, w, none);
 }
 
-// How many workgroups share a row: as many as fill the device with `wanted` workgroups, each with at least two
-// tiles per wave, and so many that a part's marks fit in LDS.
+// How many workgroups share a row: below kSharedRows rows as many as make kSharers in all, each with at least two tiles
+// per wave, and always so many that a part's marks fit in LDS. Shared rows take a kernel more. Kernel times from graphs, us, shared / whole,
+// bf16 rows of 128,256: 1 row, the k largest 13 / 15, the loss 11 / 16, with its gradient 16 / 25; 64 rows 15 / 18, 15 / 18,
+// 25 / 27; 100 rows 19 / 18, 18 / 19, 31 / 28; 255 rows 25 / 20, 24 / 21, 47 / 38. 100 fp32 rows 21 / 25, 21 / 23, 39 / 37. Narrow rows
+// gain little or lose: one of 32,768 9.6 / 10.2, 11.2 / 11.6, 15.5 / 18.1, one of 8,192 9.4 / 7.0, 11.1 / 9.4, 16.9 / 13.1. With 256 sharers the
+// losses and gradients of 64 rows took 16 and 28, with 4,096 15 and 25, their k largest 21.
+constexpr int64_t kSharedRows = 96, kSharers = 1024;
 constexpr uint32_t kMarked = 1u << 18;  // columns
-static uint32_t row_parts(const emu_logits_t* l, uint32_t V, int waves, int64_t wanted) {
+static uint32_t row_parts(const emu_logits_t* l, uint32_t V, int waves) {
   const uint32_t unit = uint32_t(waves) * 2 * (l->dtype == EMU_BF16 ? kTile<bf16_t> : kTile<float>);
   const uint32_t most = std::min((V + unit - 1) / unit, kMaxSplits);
+  const int64_t wanted = l->rows < kSharedRows ? kSharers : 1;
   const int64_t want = l->rows ? (wanted + l->rows - 1) / l->rows : 1;
   return std::max(uint32_t(std::min<int64_t>(want, most)), (V + kMarked - 1) / kMarked);
 }
@@ -1640,10 +1648,10 @@ static void by_types(int32_t in, int32_t out, F f) {
 
 constexpr int kPartWaves = 4;  // of a workgroup that has a part of a row
 
-// 4,096 rows of 128,256: 4 / 8 / 16 waves 224 / 210 / 280 us
+// 4,096 rows of 128,256: 4 / 8 / 16 waves 217 / 198 / 277 us
 static int top_waves(uint32_t n_tiles) { return std::min(row_waves(n_tiles), 8); }
-static uint32_t topk_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kTopParts, l->rows < 512 ? 1024 : 1); }
-static uint32_t distill_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kPartWaves, l->rows < 256 ? 1024 : 1); }
+static uint32_t topk_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kTopParts); }
+static uint32_t distill_parts(const emu_logits_t* l, uint32_t V) { return row_parts(l, V, kPartWaves); }
 
 // The workspace of the distillation calls.
 struct DistillWorkspace {
@@ -1671,7 +1679,7 @@ constexpr int64_t kPreparedLossRows = 1024, kPreparedGradRows = 256;
 // Whether k_distill_resident takes these rows. Reading them again instead costs less than it looks: the second read of the rows in work comes
 // from the last-level cache, and nothing waits for a row's turn. Registers pay where
 //  * there is no tail (its marks and second statistics spilled: 4,096 bf16 rows of 128,256 took 529 us held, 495 read again) and
-//    the gradient is no wider than the logits (bf16 to fp32, 2 GiB: 558 to 561 us held, 507 to 556 read again);
+//    the gradient is no wider than the logits (bf16 to fp32, 2 GiB: rows of 32,704 593 us held, 524 read again, of 128,448 558 and 556);
 //  * a wave holds enough of them: rows of 4,032 bf16 columns (8 tiles) took 989 us held, 555 read again, 1 GiB in all; 40,896
 //    (80 tiles, 8 waves of 10) 497 and 477 at 2 GiB, 51,136 (13 a wave) 477 and 485; fp32 from 64 tiles on (20,416, 80 tiles:
 //    235 and 251 at 1 GiB, 12,224, 48 tiles: 254 and 267, but 158 and 153 at half of it);
