@@ -162,11 +162,11 @@ template <typename T> using Reader = Cursor<T, kTile<T>>;
 constexpr int kScanU = 2;  // tiles that a wave adds up at a time
 
 // A tile that is not wholly in one shard and below V. Where shards are no shorter than a tile it lies in two at
-// most, and only a vector across their border goes by element (WHOLE: there is none).
-template <typename T, int POL, bool WHOLE = false>
+// most, and only a vector across their border goes by element.
+template <typename T, int POL>
 __device__ __forceinline__ v4u load_border(const Logits& l, const Reader<T>& at, uint32_t lane) {
   const uint32_t v = at.c + lane * kE<T>, lo = at.lo + lane * kE<T>;
-  if (!WHOLE && (l.cols < kTile<T> || (lo < l.cols && lo + kE<T> > l.cols))) return load_edge<T, POL>(l, at.row_off, v);
+  if (l.cols < kTile<T> || (lo < l.cols && lo + kE<T> > l.cols)) return load_edge<T, POL>(l, at.row_off, v);
   v4u x = {kMinusInf<T>, kMinusInf<T>, kMinusInf<T>, kMinusInf<T>};
   if (v >= l.V) return x;
   x = ld16_any<POL>(lo >= l.cols ? at.other(l) : at.base, lane * 16);
@@ -230,13 +230,13 @@ __device__ void store_edge(const Logits& l, uint64_t row_off, uint32_t v, const 
   }
 }
 
-// The tile at `at`, N columns a lane. WHOLE: no vector crosses a shard's end.
-template <typename TO, int POL, uint32_t N, bool WHOLE = false>
+// The tile at `at`, N columns a lane.
+template <typename TO, int POL, uint32_t N>
 __device__ __forceinline__ void store_tile(const Logits& l, const Cursor<TO, 64 * N>& at, uint32_t lane, const float (&f)[N]) {
   uint8_t* base = at.base;
   if (!at.one(l, 1)) {
     const uint32_t lo = at.lo + lane * N;
-    if (!WHOLE && (l.cols < 64 * N || (lo < l.cols && lo + N > l.cols))) return store_edge<TO, POL, N>(l, at.row_off, at.c + lane * N, f);
+    if (l.cols < 64 * N || (lo < l.cols && lo + N > l.cols)) return store_edge<TO, POL, N>(l, at.row_off, at.c + lane * N, f);
     if (at.c + lane * N >= l.Vp) return;
     if (lo >= l.cols) base = at.other(l);
   }
@@ -407,7 +407,9 @@ constexpr int kListed = 512;                           // biases of a slice held
 // Of a history's capacity: up to it 512 threads take 8,192 columns, beyond it 1,024 threads 16,384, so that half as many
 // workgroups go over a history. 256 rows of 128,256, histories of 62% of the capacity on average, us: 8,192 tokens bf16 42 / 44, fp32
 // 60 / 61; 16,384 48 / 48 and 66 / 66; 32,768 58 / 55 and 77 / 72 (256 rows of 32,768 27 / 20). The host knows the capacity
-// alone: a buffer of the model's longest sequence that holds short ones pays up to 3 us of 34 for the long form.
+// alone: a buffer of the model's longest sequence that holds short ones pays up to 3 us of 34 for the long form. The sizes: 512
+// threads on 8,192 columns took 14.8 us for 64 rows with histories of 2,500 (256 threads 15.4); 1,024 threads on 16,384 took
+// 73 us for 256 rows with 20,480 on average (on 32,768 77, 512 threads 84).
 constexpr int32_t kLongHistory = 8192;
 
 template <typename TI, typename TO, int NT, uint32_t SLICE>
@@ -921,15 +923,14 @@ __device__ __forceinline__ Stored fetch_teacher(const emu_teacher_t& te, uint64_
   return {uint32_t(f.col) < V ? f.col : -1, f.value};
 }
 
-// Logits are read in columns [z0, z1). rest: the mass outside the list (0 without a tail); none: without a tail
-// nothing is listed.
+// rest: the mass outside the list (0 without a tail); none: without a tail nothing is listed.
 template <typename T, int NW>
-__device__ __forceinline__ Entry take_teacher(DistillLds<NW>& t, Stored f, const emu_teacher_t& te, uint64_t r, const Logits& l, uint32_t z0,
-                                              uint32_t z1, float* rest, bool* none) {
+__device__ __forceinline__ Entry take_teacher(DistillLds<NW>& t, Stored f, const emu_teacher_t& te, uint64_t r, const Logits& l, float* rest,
+                                              bool* none) {
   static_assert(NW * 64 >= kMaxTeacher, "one entry per thread");
   const int j = threadIdx.x;
   Entry e = {f.col, 0.0f, -kInf};
-  if (e.col >= 0 && uint32_t(e.col) >= z0 && uint32_t(e.col) < z1) e.z = widen(*column<T>(l, r * l.row_bytes, e.col));
+  if (e.col >= 0) e.z = widen(*column<T>(l, r * l.row_bytes, e.col));
   const double value = e.col >= 0 ? double(f.value) : -double(kInf);
   double top = 0.0;
   if (!te.tail) {
@@ -1270,7 +1271,7 @@ __global__ __launch_bounds__(NW * 64) void k_distill(Logits in, Logits grad, emu
     const Running run = block_joined<NW>(scan<TI, NW, TAIL, GRAD ? POL_PLAIN : POL_NT>(in, off, row, c1, bits), t.run, c1);
     if (!teacher) {
       bool none;
-      e = take_teacher<TI, NW>(t, f, te, r, in, 0, in.V, &rest, &none);
+      e = take_teacher<TI, NW>(t, f, te, r, in, &rest, &none);
       if (none) rest = -1.0f;
     } else {
       e = {f.col, f.value, -kInf};
@@ -1476,7 +1477,7 @@ __global__ __launch_bounds__(NW * 64) void k_distill_join(Logits in, emu_teacher
   if (w == 0.0f) return write_row(loss, stats, r, 0.0f, kSkipped);
   float rest, value;
   bool none;
-  const Entry e = take_teacher<T, NW>(t, fetch_teacher(te, r, in.V), te, r, in, 0, in.V, &rest, &none);
+  const Entry e = take_teacher<T, NW>(t, fetch_teacher(te, r, in.V), te, r, in, &rest, &none);
   const Running run = wave_joined(lane < parts ? part[uint64_t(blockIdx.x) * parts + lane] : Running{-kInf, 0.0f}, c1);
   const Stats st = finish<T, NW, TAIL>(in, r * in.row_bytes, run, e, rest, te.k, c1, t, &value);
   write_row(loss, stats, r, value * w, st);
