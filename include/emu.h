@@ -438,7 +438,7 @@ int emu_logits_workspace(const emu_logits_t* logits, int32_t k, uint64_t* bytes)
 
 /* Penalties for repeated tokens, biases and grammar masks. For column v < V of row r, with x the logit, c how
  * often v occurs in tokens[prompt_len, seq_len) and s whether it occurs in tokens[0, seq_len):
- *   x1 = s ? (x > 0 ? x / theta : x * theta) : x
+ *   x1 = s ? (x > 0 ? x / theta : x * theta) : x        (x / theta is x times the rounded 1 / theta: 2^-126 <= theta <= 2^126)
  *   x2 = x1 - (alpha_f * c + alpha_p * (c > 0))
  *   x3 = x2 + the sum of v's biases, in list order
  *   out = allowed by row r's mask ? x3 : -infinity
@@ -465,12 +465,16 @@ int emu_logits_topk(const emu_logits_t* in, int32_t k, float temperature, int32_
  *           L = sum_J p_j (log p_j - log q_j) + p_R (log p_R - log q_R)
  *           dL/dz_v = (q_v - p_v) / tau inside J, q_v (1 - p_R / q_R) / tau outside
  * Terms with p = 0 are 0. A column listed twice holds the sum of its entries' probabilities. With tail 0 a row
- * without an entry, or whose values are all -infinity, has L = 0 and gradient 0. Where p > 0 meets q = 0, L is
+ * without an entry, or whose values are all -infinity, has L = 0 and gradient 0. With tail 1 the listed probabilities
+ * are expected to sum to 1 at most, but for the rounding of their logarithms: the gradient takes sum_J p_j + p_R as 1.
+ * Columns with exp((z_v - m)/tau) below 2^-126, m the row's largest logit, may count as 0. Where p > 0 meets q = 0, L is
  * +infinity and the gradient keeps its finite part (q_R < 2^-100: the factor outside J is 1); against q_R = 0 a p_R below
  * 2^-20, which the rounding of fp32 log-probabilities leaves, counts as 0.
  * d_loss[r] = w_r L_r. With grad (or NULL), its shards get w_r dL/dz, and 0 in every column from V on. d_stats
  * [rows][4], 16-byte aligned: lse of z/tau, the factor 1 - p_R/q_R (1 without a tail), the row's largest logit m and
- * sum exp((z - m)/tau). A row with w_r = 0 has loss and gradient 0, is not read, and has NaN for its statistics. */
+ * sum exp((z - m)/tau). A row with w_r = 0 has loss and gradient 0, is not read, and has NaN for its statistics. A row that
+ * holds a NaN or +infinity has NaN for its lse, and for loss and gradient where it has an entry or a tail (its m is then any
+ * of its logits, or -infinity). */
 int emu_distill(const emu_logits_t* student, const emu_teacher_t* teacher, float* d_loss, float* d_stats,
                 const emu_logits_t* grad, void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
 
