@@ -887,7 +887,7 @@ __global__ __launch_bounds__(kTopParts * 64) void k_topk_join(Logits in, uint32_
 // may be written before every reader of the row is done: hence the kernel between).
 // The gradient is coef * exp((z - m) / tau), but for the listed columns, whose gradients come from their entries'
 // threads by way of LDS. 4,096 rows of 128,256 in bf16, all with a weight: the loss 195 to 204 us
-// (5.2 to 5.4 TB/s), the loss with the gradient 426 to 430 (4.9 TB/s), the gradient alone 390 over four shards and 364
+// (5.2 to 5.4 TB/s), the loss with the gradient 422 to 430 (4.9 TB/s), the gradient alone 390 over four shards and 364
 // in one (5.4 and 5.8 TB/s). With a tail the scan leaves out the listed columns (a bit each in LDS), so that a small
 // mass outside the list is a sum of its own and no difference.
 
@@ -1677,8 +1677,8 @@ struct DistillWorkspace {
 // With the gradient: 38 against 40 for 255 of 128,256, 62 against 58 for 384; 24 against 27 for 511 of 32,768.
 constexpr int64_t kPreparedLossRows = 1024, kPreparedGradRows = 256;
 
-// Whether k_distill_resident takes these rows. Reading them again instead costs less than it looks: the second read of the rows in work comes
-// from the last-level cache, and nothing waits for a row's turn. Registers pay where
+// Whether k_distill_resident takes these rows. Reading them again (k_distill) costs less than it looks: the L2 still has a part
+// of a row (28% of 201 KB), the last-level cache most of the rest by the times, and no row waits for another. Registers pay where
 //  * there is no tail (its marks and second statistics spilled: 4,096 bf16 rows of 128,256 took 529 us held, 495 read again) and
 //    the gradient is no wider than the logits (bf16 to fp32, 2 GiB: rows of 32,704 593 us held, 524 read again, of 128,448 558 and 556);
 //  * a wave holds enough of them: rows of 4,032 bf16 columns (8 tiles) took 989 us held, 555 read again, 1 GiB in all; 40,896

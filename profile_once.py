@@ -14,6 +14,8 @@ and N written), which calibrates FETCH_SIZE / WRITE_SIZE. Workloads (--workload)
            same source and destination pages, --repeat times each, alternating.
   receiver 8B TP2 PP2 source set packed into 2^28-byte buckets (emu_pack_buckets, source side), then
            the receiver plan (emu_plan_from_buckets) resharding those buckets into TP4 PP1 tensors.
+  logits   every listed case of perf/operators.py (the operators on an LM head's logits), --repeat passes each, over
+           three sets of inputs in turn.
 
 Example (from /tmp with TMPDIR=/tmp):
 
@@ -147,9 +149,27 @@ def receiver_workload(torch, emu, device_fill):
           f"calibration copies {n} B", flush=True)
 
 
+def logits_workload(torch, repeat):
+    from perf import operators
+
+    operators.own = True
+    a, b = (torch.zeros(1 << 30, dtype=torch.uint8, device="cuda") for _ in range(2))
+    n = calibrate(torch, [a], [b])
+    print(f"profile_once: calibration copies {n} B", flush=True)
+    for case in operators.listed():
+        states = [operators.prepare(case, seed) for seed in range(3)]
+        torch.cuda.synchronize()
+        for i in range(repeat):
+            operators.run(states[i % 3])
+        torch.cuda.synchronize()
+        print(f"profile_once: {repeat} x {case['name']}, {operators.work(case)['bytes']:.6g} B each", flush=True)
+        del states
+        torch.cuda.empty_cache()
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
-    ap.add_argument("--workload", choices=["main", "shifted", "formats", "receiver"], default="main")
+    ap.add_argument("--workload", choices=["main", "shifted", "formats", "receiver", "logits"], default="main")
     ap.add_argument("--repeat", type=int, default=1)
     args = ap.parse_args()
     import torch
@@ -164,6 +184,8 @@ def main():
         shifted_workload(torch, emu, device_fill, args.repeat)
     elif args.workload == "receiver":
         receiver_workload(torch, emu, device_fill)
+    elif args.workload == "logits":
+        logits_workload(torch, args.repeat)
     else:
         formats_workload(torch, emu, device_fill, args.repeat)
 
