@@ -1673,7 +1673,7 @@ struct DistillWorkspace {
 };
 
 // Below, the row's own workgroup takes its teacher, a launch less. The loss alone: 33 us against 34 (prepared) for 511
-// bf16 rows of 128,256, 57 against 53 for 1,000; narrow rows gain less from the preparation: 36 against 39 for 2,048 of 32,768.
+// bf16 rows of 128,256, 57 against 53 for 1,000; narrow rows lose by the preparation: 36 against 39 for 2,048 of 32,768.
 // With the gradient: 38 against 40 for 255 of 128,256, 62 against 58 for 384; 24 against 27 for 511 of 32,768.
 constexpr int64_t kPreparedLossRows = 1024, kPreparedGradRows = 256;
 
